@@ -2,6 +2,7 @@
 // sequencing of one decoder pass (which sublayers run, on how many rows, at which positions).
 // Every step of the path runs in the kernels of kernels.cuh; the host only enqueues them.
 #include "../../include/knnssd.h"
+#include "host_common.cuh"
 #include "kernels.cuh"
 #include "linear_stream.cuh"
 #include "pass_kernel.cuh"
@@ -126,70 +127,6 @@ template <typename T> cudaError_t dev_alloc(T **p, size_t count) {
     return cudaMalloc(reinterpret_cast<void **>(p), count * sizeof(T));
 }
 
-// ---- scratch of the stand-alone operators --------------------------------------------------------------------------
-// One memory pool per device that keeps at most kPoolKeep bytes between calls (what it holds beyond that goes back to the
-// driver at every synchronisation, all of it when a context is destroyed): a cudaMalloc / cudaFree pair cost 100 .. 1000 us
-// a call, next to kernels of 10 .. 50 us.  Allocations are ordered on the caller's stream, so any number of threads and
-// streams may call at once.
-// 96 MB hold the largest scratch of a contraction in pieces (prefill_host.cuh: 72 MB of chunk sums) and the planes of its rows: with
-// 64, knnssd_gemm_split over 5120 x 13824 weights mapped memory on every call (77 rows 336 us, with 96 129; 1024 rows 488, 275).
-constexpr unsigned long long kPoolKeep = 96ull << 20;
-
-struct DevicePools {
-    std::mutex mu;
-    cudaMemPool_t pool[64] = {};
-    bool tried[64] = {};
-    // The pool of the current device; nullptr where the device has none.
-    cudaMemPool_t current() {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-        std::lock_guard<std::mutex> lock(mu);
-        if (!tried[dev]) {
-            tried[dev] = true;
-            int has = 0;
-            cudaMemPoolProps props{};
-            props.allocType = cudaMemAllocationTypePinned;
-            props.location.type = cudaMemLocationTypeDevice;
-            props.location.id = dev;
-            unsigned long long keep = kPoolKeep;
-            if (cudaDeviceGetAttribute(&has, cudaDevAttrMemoryPoolsSupported, dev) != cudaSuccess || !has ||
-                cudaMemPoolCreate(&pool[dev], &props) != cudaSuccess)
-                pool[dev] = nullptr;
-            else
-                cudaMemPoolSetAttribute(pool[dev], cudaMemPoolAttrReleaseThreshold, &keep);
-            cudaGetLastError();
-        }
-        return pool[dev];
-    }
-};
-DevicePools &device_pools() {
-    static DevicePools *pools = new DevicePools();      // never destroyed: a thread may still call at process exit
-    return *pools;
-}
-
-// The buffers of one call.  They are given back in stream order when it ends, whichever way it ends.
-struct Scratch {
-    cudaStream_t s;
-    cudaMemPool_t pool;
-    std::vector<void *> held;
-    explicit Scratch(cudaStream_t stream) : s(stream), pool(device_pools().current()) {}
-    Scratch(const Scratch &) = delete;
-    template <typename T> bool get(T **p, size_t count) {
-        void *q = nullptr;
-        const cudaError_t e = pool ? cudaMallocFromPoolAsync(&q, count * sizeof(T), pool, s) : cudaMalloc(&q, count * sizeof(T));
-        if (e != cudaSuccess) { cudaGetLastError(); return false; }
-        held.push_back(q);
-        *p = static_cast<T *>(q);
-        return true;
-    }
-    ~Scratch() {
-        for (void *q : held) {
-            if (pool) cudaFreeAsync(q, s);
-            else cudaFree(q);
-        }
-    }
-};
-
 // `n` words of pinned memory per host thread, which kernels read arguments from and write results to: the calls that
 // use them synchronise before they return.  At least kHostWords are kept from call to call, at most 1 MB; nullptr if they cannot be
 // had or would be more.
@@ -240,22 +177,6 @@ template <typename WT> void launch_linear_t(const LinearArgs &a, int grid, cudaS
 
 // Set by the streaming kernel of knnssd_linear if one of its bounded waits ever gives up (never in normal operation).
 __device__ int g_stream_err;
-
-constexpr int kMaxDevices = 64;
-
-// Index of the current device in the per-device tables below (0 if it cannot be read or is out of range).
-int current_device_slot() {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
-    return dev;
-}
-
-// Multiprocessors of the current device.
-int sm_count() {
-    int dev = 0, n = 148;
-    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    return n;
-}
 
 // Address of the word on the CURRENT device that the launches of knnssd_linear report to (every device that loads the library has
 // its own copy).  Sessions and the operators that synchronise have words of their own: a word that several callers read and clear
