@@ -395,6 +395,83 @@ knnssd_status knnssd_cosine_top1(const float *query_dev, const float *anchors_de
 knnssd_status knnssd_cosine_top1_static(const float *query_dev, const float *anchors_dev, int n, int d, int *best,
                                         float *cosine, void *cuda_stream);
 
+/* ---- many requests on one paged K/V cache ----
+ *
+ * The session above serves one request from one contiguous cache.  These operators serve a program that keeps the caches of many requests
+ * in pages of one pool and drafts, verifies (k + 1 new rows per request) or reads prompts for all of them at once.
+ *
+ * A layer's pool is k_pages, v_pages DEVICE [n_pages][n_kv_heads][page_size][head_dim], fp32 or bf16; page_size is a power of two, 16 or more
+ * (else KNNSSD_ERR_SHAPE).  Request b's positions lie in the pages that row b of the block table [n_requests][max_pages] names: page id
+ * table[b][p / page_size], place p % page_size.  A slot is id * page_size + place.  lens[b]: positions request b holds (committed; the new
+ * rows are behind them).  All of these are DEVICE int32, so that a step's shapes need not be known on the host: max_rows and n_rows are
+ * the room there is, row_start[n_requests] the rows there are.
+ * All four calls are asynchronous on the stream and take what scratch they need from the pool; they may be captured.  Pointers are
+ * 16-byte aligned where 16-byte values are read (else KNNSSD_ERR_SHAPE).  dtype / cache_dtype: 0 fp32, 1 bf16; bf16 rows need a bf16 cache.
+ * head_dim is 64 or 128 and n_heads a multiple of n_kv_heads (query head h reads K/V head h n_kv_heads / n_heads), else KNNSSD_ERR_SHAPE.
+ */
+
+/*
+ * The pages of one step, and where its rows go.  Request b holds, after the call, exactly the pages of its lens[b] + fresh[b] positions; with
+ * fresh[b] = -1 it has ended and holds none.  Surplus pages (drafts that were rejected, requests that ended) are pushed on the free stack
+ * and -1 is written in their place, then missing pages are popped from its top, both in request and page order.
+ *   lens_dev [n_requests], fresh_dev [n_requests] (>= -1)     in
+ *   owned_dev [n_requests], table_dev [n_requests][max_pages], free_pages_dev [n_pages], free_count_dev [1]   in and out
+ *   row_start_dev [n_requests + 1]  out: the first row of each request, their number last
+ *   row_request_dev, row_pos_dev, row_slot_dev [max_rows]  out: request, position lens[b] + i and slot of each row; -1 behind the last row
+ *   info_dev [4]  out: rows, pages taken, pages given back, and 0 or what is wrong: 1 too few free pages, 2 a request needs more than
+ *                 max_pages, 4 more than max_rows rows, 8 a length, count or fresh[b] out of range.  If anything is, nothing of the state
+ *                 has changed and there are no rows (row_start all 0).
+ * At most KNNSSD_MAX_REQUESTS requests, n_requests * max_pages, n_pages * page_size and 2 * (max_pages + 1) * page_size below 2^31: else
+ * KNNSSD_ERR_CAPACITY.
+ */
+#define KNNSSD_MAX_REQUESTS 8192
+knnssd_status knnssd_page_tables(const int *lens_dev, const int *fresh_dev, int n_requests, int page_size, int max_pages,
+                                 int n_pages, int *owned_dev, int *table_dev, int *free_pages_dev, int *free_count_dev,
+                                 int max_rows, int *row_start_dev, int *row_request_dev, int *row_pos_dev,
+                                 int *row_slot_dev, int *info_dev, void *cuda_stream);
+
+/*
+ * Rotary embedding of new rows, and their K and V into the pages.  Row r of qkv is [n_heads + 2 n_kv_heads][head_dim], rows row_stride
+ * elements apart (a multiple of 16 bytes); with (c, s) = cos_sin[row_pos[r]][i], dimensions i and i + head_dim / 2 of its q and k heads become
+ * c x[i] - s x[i + hd/2] and c x[i + hd/2] + s x[i], in fp32.
+ *   cos_sin_dev  DEVICE fp32 [n_positions][head_dim / 2][2]
+ *   q_dev        DEVICE [n_rows][n_heads][head_dim], dtype: the rotated q; zeros for a row whose position is outside [0, n_positions)
+ *   k_pages_dev, v_pages_dev  DEVICE, cache_dtype (rounded to nearest even): row r's go to row_slot[r]; nothing is stored for a row
+ *                whose position or slot is out of range (-1: padding).  Two rows of one call may not have the same slot.
+ */
+knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, long long row_stride, int n_heads,
+                                  int n_kv_heads, int head_dim, const float *cos_sin_dev, int n_positions,
+                                  const int *row_pos_dev, const int *row_slot_dev, int page_size, int n_pages, void *q_dev,
+                                  void *k_pages_dev, void *v_pages_dev, int cache_dtype, void *cuda_stream);
+
+/*
+ * Attention of the new rows over the pages: row i of request b (row row_start[b] + i of q) looks at the positions 0 .. lens[b] + i, whose K
+ * and V - its own among them - are in the pages.  out = sum_j softmax_j(scale q . k_j) v_j.
+ *   q_dev    DEVICE [n_rows][n_heads][head_dim], rows q_stride elements apart;  out_dev DEVICE [n_rows][n_heads][head_dim], dtype
+ *   max_fresh  the most rows a request has in this call, 0 if the host does not know: which kernels are launched goes by it, never the result
+ * Positions whose page id is outside [0, n_pages) are not seen; a row that sees nothing gives zeros, and so do rows at and behind
+ * row_start[n_requests].  What a row does not see never reaches it, not even NaN.  fp32 rows: 24-bit products, fp32 sums; bf16 rows: the softmax
+ * weights are rounded to bf16 for the product with V.  Runs of positions that go to one warp follow from all lengths of the call: a row's
+ * last bits depend on the company it has, not on chance.
+ */
+knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, long long q_stride, int n_heads,
+                                     int n_kv_heads, int head_dim, const void *k_pages_dev, const void *v_pages_dev,
+                                     int cache_dtype, int page_size, int n_pages, const int *table_dev, int max_pages,
+                                     const int *lens_dev, const int *row_start_dev, int n_requests, int max_fresh, float scale,
+                                     void *out_dev, void *cuda_stream);
+
+/*
+ * Causal attention over whole prompts, packed one behind the other: row i of prompt b (row row_start[b] + i) looks at rows row_start[b] ..
+ * row_start[b] + i.  Prompts may be empty.
+ *   q_dev, k_dev, v_dev  DEVICE [n_rows][heads][head_dim] of one type, rows *_stride elements apart (views of one map's output serve)
+ *   out_dev              DEVICE [n_rows][n_heads][head_dim], same type
+ * Rounding, empty rows and rows behind the last prompt as in knnssd_paged_attention.
+ */
+knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, const void *v_dev, int dtype, int n_rows,
+                                      long long q_stride, long long k_stride, long long v_stride, int n_heads, int n_kv_heads,
+                                      int head_dim, const int *row_start_dev, int n_requests, float scale, void *out_dev,
+                                      void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

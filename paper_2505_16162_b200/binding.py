@@ -25,7 +25,7 @@ EXPORTS = ["knnssd_init", "knnssd_destroy", "knnssd_prefill", "knnssd_select_ski
            "knnssd_set_pending", "knnssd_mask_objective", "knnssd_get_stats", "knnssd_last_error", "knnssd_time_pass", "knnssd_trace_pass", "knnssd_linear",
            "knnssd_gemm_split", "knnssd_linear_tc", "knnssd_build_anchors", "knnssd_cosine_top1", "knnssd_cosine_top1_static",
            "knnssd_debug_barrier_timeout", "knnssd_filtered_probs", "knnssd_sample_token", "knnssd_spec_accept",
-           "knnssd_decode_sampled"]
+           "knnssd_decode_sampled", "knnssd_page_tables", "knnssd_rotary_store", "knnssd_paged_attention", "knnssd_packed_attention"]
 
 
 class KnnssdError(RuntimeError):
@@ -57,7 +57,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2505_16162_b200.build` "
                           "(there is no CPU fallback)")
     lib = C.CDLL(LIB_PATH)
-    P, I, F = C.c_void_p, C.c_int, C.c_float
+    P, I, F, L = C.c_void_p, C.c_int, C.c_float, C.c_longlong
     PI, PF = C.POINTER(C.c_int), C.POINTER(C.c_float)
     sigs = {
         "knnssd_init": (I, [C.POINTER(Config), C.POINTER(Weights), P, P, P, C.POINTER(P)]),
@@ -89,6 +89,10 @@ def _load():
         "knnssd_sample_token": (I, [P, I, F, PI, P]),
         "knnssd_spec_accept": (I, [P, P, P, I, I, P, F, PI, PI, P]),
         "knnssd_decode_sampled": (I, [P, I, I, F, F, P, I, P, PI, P, C.POINTER(Stats)]),
+        "knnssd_page_tables": (I, [P, P, I, I, I, I, P, P, P, P, I, P, P, P, P, P, P]),
+        "knnssd_rotary_store": (I, [P, I, I, L, I, I, I, P, I, P, P, I, I, P, P, P, I, P]),
+        "knnssd_paged_attention": (I, [P, I, I, L, I, I, I, P, P, I, I, I, P, I, P, P, I, I, F, P, P]),
+        "knnssd_packed_attention": (I, [P, P, P, I, I, L, L, L, I, I, I, P, I, F, P, P]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -258,6 +262,148 @@ def knnssd_cosine_top1_static(query: torch.Tensor, anchors: torch.Tensor):
     if rc:
         raise KnnssdError(rc, "knnssd_cosine_top1_static")
     return best.value, cs.value
+
+
+# ---- many requests on one paged K/V cache ----
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _i32(t: torch.Tensor, shape, what: str) -> int:
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous CUDA int32 tensor of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, what: str) -> int:
+    """Address of [rows][heads][head_dim] values whose rows are dense; the rows may be any distance apart."""
+    if t.dim() != 3 or not t.is_cuda or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{what} must be a CUDA tensor [rows][heads][head_dim] whose heads are contiguous")
+    return t.data_ptr()
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _pages(k: torch.Tensor, v: torch.Tensor):
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not (k.is_cuda and v.is_cuda and k.is_contiguous() and v.is_contiguous()):
+        raise ValueError("k_pages and v_pages must be contiguous CUDA tensors [n_pages][n_kv_heads][page_size][head_dim] of one type")
+    return k.shape
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _same_device(*tensors: torch.Tensor):
+    first = tensors[0].device
+    for t in tensors:
+        if t.device != first:
+            raise ValueError("all tensors of a call must be on one device")
+
+
+def _call(fn, name: str, device: torch.device, *args):
+    """fn(*args, stream) on `device`'s current stream."""
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if rc:
+        raise KnnssdError(rc, name)
+
+
+def knnssd_page_tables(lens: torch.Tensor, fresh: torch.Tensor, owned: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
+                       free_count: torch.Tensor, page_size: int, row_start: torch.Tensor, row_request: torch.Tensor, row_pos: torch.Tensor,
+                       row_slot: torch.Tensor, info: torch.Tensor) -> None:
+    """The pages of one step and the slots of its rows, on the GPU; all tensors int32, contiguous.  lens, fresh [B] in; owned [B], table
+    [B][max_pages], free_pages [n_pages], free_count [1] in and out; row_start [B + 1], row_request / row_pos / row_slot [max_rows], info [4]
+    (rows, pages taken, pages given back, what is wrong) out.  See the header for the order pages go in."""
+    if lens.dim() != 1 or table.dim() != 2 or free_pages.dim() != 1 or row_pos.dim() != 1:
+        raise ValueError("lens, free_pages and the rows' maps have one dimension, table two")
+    B, n_pages, rows, max_pages = lens.shape[0], free_pages.shape[0], row_pos.shape[0], table.shape[1]
+    _same_device(lens, fresh, owned, table, free_pages, free_count, row_start, row_request, row_pos, row_slot, info)
+    _call(_lib.knnssd_page_tables, "knnssd_page_tables", lens.device, _i32(lens, (B,), "lens"), _i32(fresh, (B,), "fresh"), B, page_size, max_pages, n_pages,
+          _i32(owned, (B,), "owned"), _i32(table, (B, max_pages), "table"), _i32(free_pages, (n_pages,), "free_pages"), _i32(free_count, (1,), "free_count"), rows,
+          _i32(row_start, (B + 1,), "row_start"), _i32(row_request, (rows,), "row_request"), _i32(row_pos, (rows,), "row_pos"),
+          _i32(row_slot, (rows,), "row_slot"), _i32(info, (4,), "info"))
+
+
+def rotary_table(n_positions: int, head_dim: int, theta: float, device="cuda") -> torch.Tensor:
+    """(cos, sin) of position times theta^(-2 i / head_dim), fp32 [n_positions][head_dim / 2][2], angles formed in 64 bits."""
+    half = head_dim // 2
+    a = torch.arange(n_positions, device=device, dtype=torch.float64)[:, None] * theta ** (-torch.arange(half, device=device, dtype=torch.float64) / half)
+    return torch.stack([a.cos(), a.sin()], dim=-1).float().contiguous()
+
+
+def knnssd_rotary_store(qkv: torch.Tensor, cos_sin: torch.Tensor, row_pos: torch.Tensor, row_slot: torch.Tensor, k_pages: torch.Tensor,
+                        v_pages: torch.Tensor, q: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotates the q and k heads of the rows of qkv [rows][(n_heads + 2 n_kv_heads) head_dim] by their positions, puts K and V into their
+    slots and returns q [rows][n_heads][head_dim] in qkv's type."""
+    n_pages, kv, page, hd = _pages(k_pages, v_pages)
+    dtype, cache = _type(qkv, "qkv"), _type(k_pages, "k_pages")
+    if qkv.dim() != 2 or not qkv.is_cuda or qkv.stride(1) != 1 or qkv.shape[1] % hd != 0 or qkv.shape[1] // hd <= 2 * kv:
+        raise ValueError("qkv must be a CUDA tensor [rows][(n_heads + 2 n_kv_heads) head_dim] with dense rows")
+    rows, heads = qkv.shape[0], qkv.shape[1] // hd - 2 * kv
+    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 3 or cos_sin.shape[1:] != (hd // 2, 2) or not cos_sin.is_cuda or not cos_sin.is_contiguous():
+        raise ValueError("cos_sin must be a contiguous CUDA float32 tensor [positions][head_dim / 2][2]")
+    if q is None:
+        q = torch.empty((rows, heads, hd), dtype=qkv.dtype, device=qkv.device)
+    elif q.shape != (rows, heads, hd) or q.dtype != qkv.dtype or not q.is_cuda or not q.is_contiguous():
+        raise ValueError("q must be a contiguous CUDA tensor [rows][n_heads][head_dim] of qkv's type")
+    _same_device(qkv, cos_sin, row_pos, row_slot, k_pages, v_pages, q)
+    _call(_lib.knnssd_rotary_store, "knnssd_rotary_store", qkv.device, qkv.data_ptr(), dtype, rows, qkv.stride(0) if rows > 1 else qkv.shape[1], heads, kv, hd,
+          cos_sin.data_ptr(), cos_sin.shape[0], _i32(row_pos, (rows,), "row_pos"), _i32(row_slot, (rows,), "row_slot"), page, n_pages, q.data_ptr(),
+          k_pages.data_ptr(), v_pages.data_ptr(), cache)
+    return q
+
+
+def _attention_out(q: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
+    if out is None:
+        return torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if out.shape != q.shape or out.dtype != q.dtype or not out.is_cuda or not out.is_contiguous():
+        raise ValueError("out must be a contiguous CUDA tensor of q's shape and type")
+    return out
+
+
+def knnssd_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                           row_start: torch.Tensor, max_fresh: int = 0, scale: Optional[float] = None,
+                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new rows q [rows][n_heads][head_dim] over the requests' pages: row row_start[b] + i sees positions 0 .. lens[b] + i.
+    table [B][max_pages], lens [B], row_start [B + 1] int32.  max_fresh: the most rows of a request in this call, if known.  scale defaults to
+    head_dim ** -0.5."""
+    n_pages, kv, page, hd = _pages(k_pages, v_pages)
+    dtype, cache = _type(q, "q"), _type(k_pages, "k_pages")
+    qp = _rows(q, "q")
+    if q.shape[2] != hd or table.dim() != 2:
+        raise ValueError("q's head_dim must be the pages', and table must be [requests][max_pages]")
+    rows, heads, _ = q.shape
+    B, max_pages = table.shape
+    out = _attention_out(q, out)
+    _same_device(q, k_pages, v_pages, table, lens, row_start, out)
+    _call(_lib.knnssd_paged_attention, "knnssd_paged_attention", q.device, qp, dtype, rows, _row_stride(q), heads, kv, hd, k_pages.data_ptr(), v_pages.data_ptr(),
+          cache, page, n_pages, _i32(table, (B, max_pages), "table"), max_pages, _i32(lens, (B,), "lens"), _i32(row_start, (B + 1,), "row_start"), B, max_fresh,
+          hd ** -0.5 if scale is None else scale, out.data_ptr())
+    return out
+
+
+def knnssd_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, scale: Optional[float] = None,
+                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention over packed prompts: q [rows][n_heads][head_dim], k, v [rows][n_kv_heads][head_dim] of one type, rows any distance
+    apart; prompt b is the rows row_start[b] .. row_start[b + 1] - 1.  scale defaults to head_dim ** -0.5."""
+    dtype = _type(q, "q")
+    qp, kp, vp = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    rows, heads, hd = q.shape
+    if k.shape != v.shape or k.dtype != q.dtype or v.dtype != q.dtype or k.shape[0] != rows or k.shape[2] != hd or row_start.dim() != 1 or row_start.shape[0] < 2:
+        raise ValueError("k and v must be [rows][n_kv_heads][head_dim] of q's type, row_start [prompts + 1]")
+    B = row_start.shape[0] - 1
+    out = _attention_out(q, out)
+    _same_device(q, k, v, row_start, out)
+    _call(_lib.knnssd_packed_attention, "knnssd_packed_attention", q.device, qp, kp, vp, dtype, rows, _row_stride(q), _row_stride(k), _row_stride(v), heads,
+          k.shape[1], hd, _i32(row_start, (B + 1,), "row_start"), B, hd ** -0.5 if scale is None else scale, out.data_ptr())
+    return out
 
 
 class Session:

@@ -8,8 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libknnssd.so")
-SOURCES = ["knnssd.cu"]
-HEADERS = ["host_common.cuh", "device_common.cuh", "kernels.cuh", "linear_stream.cuh", "linear_presplit.cuh", "pass_kernel.cuh", "prefill.cuh", "prefill_host.cuh", "anchors.cuh", "linear_tc.cuh", "sampling.cuh", "small_pass.cuh", os.path.join("..", "..", "include", "knnssd.h")]
+SOURCES = ["knnssd.cu", "paged.cu"]
+HEADERS = ["host_common.cuh", "device_common.cuh", "kernels.cuh", "linear_stream.cuh", "linear_presplit.cuh", "pass_kernel.cuh", "prefill.cuh", "prefill_host.cuh", "anchors.cuh", "linear_tc.cuh", "sampling.cuh", "small_pass.cuh", "page_tables.cuh", "row_attention.cuh", os.path.join("..", "..", "include", "knnssd.h")]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-shared", "--use_fast_math=false"]
 
@@ -28,7 +28,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         flags = [f for f in NVCC_FLAGS if not f.startswith("--use_fast_math")]
         if verbose:
             flags += ["-Xptxas", "-v"]
-        cmd = [nvcc] + flags + ["-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
+        cmd = [nvcc, "--threads", str(len(SOURCES))] + flags + ["-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
         subprocess.check_call(cmd)
     return LIB
 

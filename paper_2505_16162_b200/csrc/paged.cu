@@ -1,0 +1,169 @@
+// Host side of the operators for many requests on one paged K/V cache: block tables and slot maps, rotary embedding into pages, attention
+// of new rows over pages, attention over packed prompts.  The C ABI is declared in include/knnssd.h.
+#include "../../include/knnssd.h"
+#include "host_common.cuh"
+#include "page_tables.cuh"
+#include "row_attention.cuh"
+
+#include <climits>
+#include <cmath>
+#include <cstdint>
+
+using namespace knnssd;
+
+namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool power_of_two(int v) { return v > 0 && (v & (v - 1)) == 0; }
+
+knnssd_status launched() { return cudaGetLastError() == cudaSuccess ? KNNSSD_OK : KNNSSD_ERR_CUDA; }
+
+// Dynamic shared memory of a kernel on the current device, set once per device.
+template <typename K> bool allow_smem(K kernel, int bytes, bool (&done)[kMaxDevices]) {
+    const int dev = current_device_slot();
+    if (done[dev]) return true;
+    done[dev] = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+    return done[dev];
+}
+
+template <int HD, typename QT, typename KT, bool PAGED, int MB> knnssd_status launch_rows(rowattn::Args a, cudaStream_t s) {
+    using Rg = rowattn::Ring<HD, KT>;
+    static bool configured[kMaxDevices] = {};
+    const auto kernel = rowattn::rows_kernel<HD, QT, KT, PAGED, MB>;
+    if (!allow_smem(kernel, Rg::SMEM, configured)) return KNNSSD_ERR_CUDA;
+    const int G = a.H / a.KV, most = 16 * MB;
+    a.gs = (G + (G + most - 1) / most - 1) / ((G + most - 1) / most);
+    a.subs = (G + a.gs - 1) / a.gs;
+    a.tb = most / a.gs;
+    const int ctas = sm_count(), warps = ctas * Rg::WARPS;
+    Scratch mem(s);
+    const size_t slots = (size_t)warps * rowattn::SLOTS * most;
+    if (!mem.get(&a.parts, (size_t)warps) || !mem.get(&a.ml, slots) || !mem.get(&a.o, slots * HD)) return KNNSSD_ERR_CUDA;
+    launch_chained(kernel, dim3(ctas), dim3(Rg::WARPS * 32), Rg::SMEM, s, a);
+    launch_chained(rowattn::merge_kernel<HD, QT, MB>, dim3(warps - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
+    return launched();
+}
+
+template <int HD, bool PAGED> knnssd_status launch_types(const rowattn::Args &a, int dtype, int cache_dtype, int mb, cudaStream_t s) {
+    if (dtype == 0 && cache_dtype == 0) return launch_rows<HD, float, float, PAGED, 1>(a, s);
+    if constexpr (PAGED) {
+        if (dtype == 0) return launch_rows<HD, float, bf16_t, PAGED, 1>(a, s);
+        if (mb == 1) return launch_rows<HD, bf16_t, bf16_t, PAGED, 1>(a, s);
+    }
+    return launch_rows<HD, bf16_t, bf16_t, PAGED, 2>(a, s);
+}
+
+template <int HD> void launch_rotary(const pages::RotaryArgs &a, int dtype, int cache_dtype, cudaStream_t s) {
+    const dim3 grid(a.n_rows), block(pages::ROT_NT);
+    if (dtype == 1) launch_chained(pages::rotary_store_kernel<HD, bf16_t, bf16_t>, grid, block, 0, s, a);
+    else if (cache_dtype == 1) launch_chained(pages::rotary_store_kernel<HD, float, bf16_t>, grid, block, 0, s, a);
+    else launch_chained(pages::rotary_store_kernel<HD, float, float>, grid, block, 0, s, a);
+}
+
+// Types and head counts that the attention operators and the store share.
+knnssd_status check_heads(int dtype, int cache_dtype, int n_heads, int n_kv_heads, int head_dim) {
+    if ((dtype != 0 && dtype != 1) || (cache_dtype != 0 && cache_dtype != 1) || n_heads < 1 || n_kv_heads < 1) return KNNSSD_ERR_INVALID_ARG;
+    if ((dtype == 1 && cache_dtype == 0) || (head_dim != 64 && head_dim != 128) || n_heads % n_kv_heads != 0 || n_heads > 65535) return KNNSSD_ERR_SHAPE;
+    return KNNSSD_OK;
+}
+knnssd_status check_pages(int page_size, int max_pages, int n_pages) {
+    if (page_size < 1 || max_pages < 1 || n_pages < 1) return KNNSSD_ERR_INVALID_ARG;
+    if (page_size < 16 || !power_of_two(page_size)) return KNNSSD_ERR_SHAPE;
+    if ((long long)(max_pages + 1ll) * page_size > INT_MAX / 2 || (long long)n_pages * page_size > INT_MAX) return KNNSSD_ERR_CAPACITY;
+    return KNNSSD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+knnssd_status knnssd_page_tables(const int *lens_dev, const int *fresh_dev, int n_requests, int page_size, int max_pages, int n_pages, int *owned_dev, int *table_dev,
+                                 int *free_pages_dev, int *free_count_dev, int max_rows, int *row_start_dev, int *row_request_dev, int *row_pos_dev, int *row_slot_dev,
+                                 int *info_dev, void *cuda_stream) {
+    if (!lens_dev || !fresh_dev || !owned_dev || !table_dev || !free_pages_dev || !free_count_dev || !row_start_dev || !info_dev || n_requests < 1 || max_rows < 0 ||
+        (max_rows > 0 && (!row_request_dev || !row_pos_dev || !row_slot_dev)))
+        return KNNSSD_ERR_INVALID_ARG;
+    if (const knnssd_status st = check_pages(page_size, max_pages, n_pages); st != KNNSSD_OK) return st;
+    if (n_requests > pages::MAX_REQUESTS || (long long)n_requests * max_pages > INT_MAX) return KNNSSD_ERR_CAPACITY;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+    static bool configured[kMaxDevices] = {};
+    if (!allow_smem(pages::plan_kernel, pages::plan_smem(pages::MAX_REQUESTS), configured)) return KNNSSD_ERR_CUDA;
+    pages::PlanArgs a{lens_dev, fresh_dev, n_requests, page_size, max_pages, n_pages, owned_dev, table_dev, free_pages_dev, free_count_dev, max_rows,
+                      row_start_dev, row_request_dev, row_pos_dev, row_slot_dev, info_dev, max_rows <= 4096};
+    launch_chained(pages::plan_kernel, dim3(1), dim3(pages::NT), pages::plan_smem(n_requests), s, a);
+    if (!a.rows_here) launch_chained(pages::map_rows_kernel, dim3((max_rows + pages::ROWS_NT - 1) / pages::ROWS_NT), dim3(pages::ROWS_NT), 0, s, a);
+    return launched();
+}
+
+knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, long long row_stride, int n_heads, int n_kv_heads, int head_dim, const float *cos_sin_dev,
+                                  int n_positions, const int *row_pos_dev, const int *row_slot_dev, int page_size, int n_pages, void *q_dev, void *k_pages_dev,
+                                  void *v_pages_dev, int cache_dtype, void *cuda_stream) {
+    if (n_rows < 0 || n_positions < 1) return KNNSSD_ERR_INVALID_ARG;
+    if (knnssd_status st = check_heads(dtype, cache_dtype, n_heads, n_kv_heads, head_dim); st != KNNSSD_OK) return st;
+    if (knnssd_status st = check_pages(page_size, 1, n_pages); st != KNNSSD_OK) return st;
+    if (n_rows == 0) return KNNSSD_OK;
+    if (!qkv_dev || !cos_sin_dev || !row_pos_dev || !row_slot_dev || !q_dev || !k_pages_dev || !v_pages_dev) return KNNSSD_ERR_INVALID_ARG;
+    const long long width = ((long long)n_heads + 2ll * n_kv_heads) * head_dim;
+    if (row_stride < width || row_stride % (dtype ? 8 : 4) != 0 || !aligned16(qkv_dev) || !aligned16(cos_sin_dev) || !aligned16(q_dev) || !aligned16(k_pages_dev) ||
+        !aligned16(v_pages_dev))
+        return KNNSSD_ERR_SHAPE;
+    pages::RotaryArgs a{qkv_dev, row_stride, n_rows, n_heads, n_kv_heads, n_positions, reinterpret_cast<const float2 *>(cos_sin_dev), row_pos_dev, row_slot_dev, page_size,
+                        n_pages * page_size, q_dev, k_pages_dev, v_pages_dev};
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+    if (head_dim == 128) launch_rotary<128>(a, dtype, cache_dtype, s);
+    else launch_rotary<64>(a, dtype, cache_dtype, s);
+    return launched();
+}
+
+knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, long long q_stride, int n_heads, int n_kv_heads, int head_dim, const void *k_pages_dev,
+                                     const void *v_pages_dev, int cache_dtype, int page_size, int n_pages, const int *table_dev, int max_pages, const int *lens_dev,
+                                     const int *row_start_dev, int n_requests, int max_fresh, float scale, void *out_dev, void *cuda_stream) {
+    if (n_rows < 0 || n_requests < 1 || max_fresh < 0 || !std::isfinite(scale)) return KNNSSD_ERR_INVALID_ARG;
+    if (knnssd_status st = check_heads(dtype, cache_dtype, n_heads, n_kv_heads, head_dim); st != KNNSSD_OK) return st;
+    if (knnssd_status st = check_pages(page_size, max_pages, n_pages); st != KNNSSD_OK) return st;
+    if (n_rows > INT_MAX / 2) return KNNSSD_ERR_CAPACITY;
+    if (n_rows == 0) return KNNSSD_OK;
+    if (!q_dev || !k_pages_dev || !v_pages_dev || !table_dev || !lens_dev || !row_start_dev || !out_dev) return KNNSSD_ERR_INVALID_ARG;
+    if (q_stride < (long long)n_heads * head_dim || q_stride % (dtype ? 8 : 4) != 0 || !aligned16(q_dev) || !aligned16(k_pages_dev) || !aligned16(v_pages_dev) || !aligned16(out_dev))
+        return KNNSSD_ERR_SHAPE;
+    rowattn::Args a{};
+    a.q = q_dev; a.out = out_dev; a.q_stride = q_stride;
+    a.k = k_pages_dev; a.v = v_pages_dev;
+    a.table = table_dev; a.max_pages = max_pages; a.n_pages = n_pages;
+    while ((1 << a.page_shift) < page_size) ++a.page_shift;
+    a.lens = lens_dev; a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.most = INT_MAX; a.least_run = 64;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+    const int group = n_heads / n_kv_heads, mb = max_fresh > 0 && (long long)max_fresh * group <= 16 ? 1 : 2;
+    try {
+        return head_dim == 128 ? launch_types<128, true>(a, dtype, cache_dtype, mb, s) : launch_types<64, true>(a, dtype, cache_dtype, mb, s);
+    } catch (...) { return KNNSSD_ERR_CUDA; }
+}
+
+knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, const void *v_dev, int dtype, int n_rows, long long q_stride, long long k_stride,
+                                      long long v_stride, int n_heads, int n_kv_heads, int head_dim, const int *row_start_dev, int n_requests, float scale, void *out_dev,
+                                      void *cuda_stream) {
+    if (n_rows < 0 || n_requests < 1 || !std::isfinite(scale)) return KNNSSD_ERR_INVALID_ARG;
+    if (knnssd_status st = check_heads(dtype, dtype, n_heads, n_kv_heads, head_dim); st != KNNSSD_OK) return st;
+    if (n_rows > INT_MAX / 2) return KNNSSD_ERR_CAPACITY;
+    if (n_rows == 0) return KNNSSD_OK;
+    if (!q_dev || !k_dev || !v_dev || !row_start_dev || !out_dev) return KNNSSD_ERR_INVALID_ARG;
+    const int per16 = dtype ? 8 : 4;
+    const long long kv_width = (long long)n_kv_heads * head_dim;
+    if (q_stride < (long long)n_heads * head_dim || k_stride < kv_width || v_stride < kv_width || q_stride % per16 || k_stride % per16 || v_stride % per16 || !aligned16(q_dev) ||
+        !aligned16(k_dev) || !aligned16(v_dev) || !aligned16(out_dev))
+        return KNNSSD_ERR_SHAPE;
+    rowattn::Args a{};
+    a.q = q_dev; a.out = out_dev; a.q_stride = q_stride;
+    a.k = k_dev; a.v = v_dev; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.most = INT_MAX; a.least_run = 64;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+    try {
+        return head_dim == 128 ? launch_types<128, false>(a, dtype, dtype, 2, s) : launch_types<64, false>(a, dtype, dtype, 2, s);
+    } catch (...) { return KNNSSD_ERR_CUDA; }
+}
+
+}  // extern "C"
