@@ -1,0 +1,242 @@
+// How the attention operators share their work out: items, and equal runs of their positions.
+//
+// An item is (request, block of new rows, K/V head): the rows of a block times the query heads that
+// share the head, over the positions that the block's last row sees.  The positions of all items, one item behind the other in request,
+// block and head order, are cut into equal runs, one per worker (a warp or a block of the launch), whatever the lengths.  Where an item begins follows
+// from the sums of the requests' costs and a closed form within a request, so every worker finds its own run from the lengths on the device.
+// Parts of an item that several workers have are put together by merge_kernel.
+#pragma once
+
+#include "device_common.cuh"
+
+namespace knnssd {
+namespace attn {
+
+constexpr int SLOTS = 2;                  // parts a worker may leave: of the item its run begins in, of the one it ends in
+
+struct Args {
+    const void *q;                        // [R][H][hd], rows q_stride elements apart
+    void *out;                            // [R][H][hd]
+    long long q_stride;
+    const void *k, *v;                    // pages [n_pages][KV][page][hd]; packed: [R][KV][hd], rows k_stride / v_stride elements apart
+    long long k_stride, v_stride;
+    const int *table;                     // [B][max_pages]
+    int max_pages, page_shift, n_pages;
+    const int *lens, *row_start;          // [B] (packed: nullptr, nothing held), [B + 1]
+    int B, R, H, KV;
+    float scale_log2;                     // scale log2 e: the softmax runs in powers of two
+    int gs, subs, nvh;                    // query heads of an item; items that share a K/V head's rows (heads of a group / gs); KV subs
+    int tb;                               // new rows of a block (of half a block, where blocks have two halves)
+    int most;                             // requests of up to this many new rows are the rows kernel's, the others the tensor kernel's
+    int extra;                            // positions that an item's beginning and end cost
+    int least_run;                        // positions a worker takes at least
+    int clear;                            // rows that no request has are this launch's to clear
+    // parts of items: what worker w knows of the item its run begins in, and its parts' (m, l) [w][SLOTS][rows] and o [w][SLOTS][rows][hd]
+    struct Part *parts;
+    float2 *ml;
+    float *o;
+    int *err;
+};
+
+// first: no run before this one begins within the item; [from, to): the run's positions of it; start: the item (-1: none)
+struct Part { long long start; int first, kv, from, to, row0, rows, vh, paired; };
+
+// A request's new rows n, what it held before, the block's rows tb and the items nvh per block.  HALVES: a block has two halves of a.tb rows each;
+// where a request has no more than one of them, the halves take two heads instead.
+struct Request { int n, held, row0, tb, nvh; long long cost; };
+
+template <bool HALVES> __device__ __forceinline__ Request request_of(const Args &a, int b) {
+    Request r;
+    const int r0 = min(max(a.row_start[b], 0), a.R), r1 = min(max(a.row_start[b + 1], 0), a.R);
+    r.n = max(r1 - r0, 0);
+    r.row0 = r0;
+    r.held = a.lens ? (int)min((long long)max(a.lens[b], 0), (long long)a.max_pages << a.page_shift) : 0;
+    if (HALVES ? r.n <= a.most : r.n > a.most) r.n = 0;
+    r.tb = HALVES && r.n > a.tb ? 2 * a.tb : a.tb;
+    r.nvh = HALVES && r.n <= a.tb ? (a.nvh + 1) / 2 : a.nvh;
+    const long long whole = r.n / r.tb, left = r.n % r.tb, each = (long long)r.held + a.extra;
+    r.cost = (whole * each + r.tb * (whole * (whole + 1) / 2) + (left ? each + r.n : 0)) * r.nvh;
+    return r;
+}
+
+// An item and where it begins among all items' positions.
+template <bool HALVES> struct Item {
+    Request r;
+    int b, rb, vh, kv;                    // kv: positions that the block's last row sees
+    long long start;
+    __device__ __forceinline__ void see() { kv = r.held + min(r.tb * (rb + 1), r.n); }
+    __device__ __forceinline__ int tokens() const { return min(r.tb, r.n - rb * r.tb); }
+    __device__ __forceinline__ bool paired() const { return HALVES && r.n <= r.tb && r.tb == tb_half; }
+    int tb_half;
+    // the item behind this one; false when there is none
+    __device__ __forceinline__ bool next(const Args &a) {
+        start += kv + a.extra;
+        if (++vh < r.nvh) return true;
+        vh = 0;
+        if (++rb * r.tb < r.n) { see(); return true; }
+        rb = 0;
+        while (++b < a.B) {
+            r = request_of<HALVES>(a, b);
+            if (r.cost > 0) { see(); return true; }
+        }
+        return false;
+    }
+};
+
+// A block's view of the requests: the costs of N runs of them, summed, N threads.
+template <int N> struct Costs {
+    long long pfx[N + 1];
+    long long warp_sum[N / 32];
+};
+
+template <bool HALVES, int N> __device__ __forceinline__ void sum_costs(const Args &a, Costs<N> &c) {
+    const int tid = threadIdx.x, per = (a.B + N - 1) / N, lane = tid & 31;
+    long long v = 0;
+    if (tid < N) {
+        for (int b = tid * per; b < min((tid + 1) * per, a.B); ++b) v += request_of<HALVES>(a, b).cost;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += u;
+        }
+        if (lane == 31) c.warp_sum[tid >> 5] = v;
+    }
+    __syncthreads();
+    if (tid < N) {
+        for (int w = 0; w < tid >> 5; ++w) v += c.warp_sum[w];
+        c.pfx[tid + 1] = v;
+        if (tid == 0) c.pfx[0] = 0;
+    }
+    __syncthreads();
+}
+
+// The item that position x of all items' lies in; x < the sum.
+template <bool HALVES, int N> __device__ __forceinline__ Item<HALVES> item_at(const Args &a, const Costs<N> &c, long long x) {
+    int lo = 0, hi = N - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (c.pfx[mid + 1] > x) hi = mid; else lo = mid + 1;
+    }
+    Item<HALVES> it;
+    it.tb_half = a.tb;
+    it.start = c.pfx[lo];
+    it.b = lo * ((a.B + N - 1) / N);
+    for (;; ++it.b) {
+        it.r = request_of<HALVES>(a, it.b);
+        if (x < it.start + it.r.cost) break;
+        it.start += it.r.cost;
+    }
+    // block rb begins at nvh (rb (held + extra) + tb rb (rb + 1) / 2)
+    const long long at = x - it.start;
+    auto before = [&](long long rb) { return it.r.nvh * (rb * ((long long)it.r.held + a.extra) + it.r.tb * (rb * (rb + 1) / 2)); };
+    int r0 = 0, r1 = (it.r.n + it.r.tb - 1) / it.r.tb - 1;
+    while (r0 < r1) {
+        const int mid = (r0 + r1) >> 1;
+        if (before(mid + 1) > at) r1 = mid; else r0 = mid + 1;
+    }
+    it.rb = r0;
+    it.see();
+    it.vh = (int)((at - before(r0)) / (it.kv + a.extra));
+    it.start += before(r0) + (long long)it.vh * (it.kv + a.extra);
+    return it;
+}
+
+// The run of worker w of W, and where position x cuts an item: at the next multiple of TP of it.
+__device__ __forceinline__ long long run_start(long long total, int w, int W) { return total / W * w + total % W * w / W; }
+template <int TP, bool HALVES> __device__ __forceinline__ int cut(const Item<HALVES> &it, long long x) {
+    return (int)(x <= it.start ? 0 : min((x - it.start + TP - 1) & ~(long long)(TP - 1), (long long)it.kv));
+}
+__device__ __forceinline__ int workers_of(const Args &a, long long total, int most) { return (int)max(1ll, min((long long)most, total / a.least_run)); }
+
+// What worker w leaves for the merge about the item that its run begins in.
+template <int TP, bool HALVES> __device__ __forceinline__ void note_part(const Args &a, const Item<HALVES> &it, int w, int W, long long total, long long x0, long long x1) {
+    Part p;
+    p.start = it.start;
+    p.from = cut<TP>(it, x0); p.to = cut<TP>(it, x1); p.kv = it.kv;
+    p.first = p.from > 0 && p.from < it.kv && run_start(total, w - 1, W) <= it.start;
+    p.row0 = it.r.row0 + it.rb * it.r.tb; p.rows = it.tokens(); p.vh = it.vh; p.paired = it.paired();
+    a.parts[w] = p;
+}
+
+// Rows at and behind the last request's are nobody's: zeros.
+template <typename T> __device__ __forceinline__ void clear_tail(const Args &a, int hd, int thread, int threads) {
+    const long long row = (long long)a.H * hd, used = min(max(a.row_start[a.B], 0), a.R);
+    for (long long i = used * row + thread; i < a.R * row; i += threads) static_cast<T *>(a.out)[i] = T(0);
+}
+
+// Row r of an item's rows (ROWS, two halves of ROWS / 2 where HALVES): the new row of the block and the query head; -1 where there is none.
+template <bool HALVES, int ROWS> __device__ __forceinline__ void place_of(const Args &a, int tokens, int vh, bool paired, int r, int &token, int &head) {
+    const int half = HALVES ? r / (ROWS / 2) : 0, rr = HALVES ? r % (ROWS / 2) : r;
+    const int t = rr / a.gs, v = paired ? 2 * vh + half : vh;
+    token = t < a.tb ? t + (paired ? 0 : half * a.tb) : -1;
+    const int G = a.H / a.KV, kvh = v / a.subs, h = (v % a.subs) * a.gs + rr % a.gs;
+    if (token >= tokens || v >= a.nvh || h >= G) token = -1;
+    head = kvh * G + h;
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Items in parts.  Block (w, j) does eight rows, j 8 .., of the item that worker w's run is the first to begin within: the part of worker w - 1
+// and those behind it until the item's end, in their order.  A warp per row: its lanes share the parts' (m, l) out, then hd / 32
+// dimensions each.
+template <int HD, typename QT, bool HALVES, int ROWS>
+__global__ void __launch_bounds__(256) merge_kernel(const Args a) {
+    chain_wait();
+    const int w = blockIdx.x + 1, lane = threadIdx.x & 31;
+    const Part p = a.parts[w];
+    if (!p.first) return;
+    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
+    int token, head;
+    place_of<HALVES, ROWS>(a, p.rows, p.vh, p.paired, r, token, head);
+    if (token < 0) return;
+    // part i: of run w - 1 + i, as long as the runs begin in this item
+    auto slot = [&](int i) { return ((size_t)(w - 1 + i) * SLOTS + (i == 0 ? 1 : 0)) * ROWS + r; };
+    const int most = gridDim.x + 2 - w;
+    constexpr int D = HD / 32;
+    float o[D], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < D; ++i) o[i] = 0.f;
+    for (int i0 = 0;; i0 += 32) {
+        const int i = i0 + lane;
+        bool mine = i < most, there = mine;                          // there: not cut away
+        if (mine && i > 0) {
+            const Part *q = a.parts + w - 1 + i;
+            mine = q->start == p.start;
+            there = mine && q->from < q->to;
+        }
+        const unsigned all = __ballot_sync(0xffffffffu, mine);
+        const int n = all == 0xffffffffu ? 32 : __ffs(~all) - 1;      // lanes up to the first that is not of the item
+        there = there && lane < n;
+        const float2 v = there ? a.ml[slot(i)] : make_float2(-INFINITY, 0.f);
+        const float mn = fmaxf(m, warp_max(v.x)), base = mn == -INFINITY ? 0.f : mn;
+        const float f = exp2_approx(v.x - base), old = exp2_approx(m - base);
+        l = l * old + warp_sum(v.y * f);
+#pragma unroll
+        for (int j = 0; j < D; ++j) o[j] *= old;
+        m = mn;
+        const unsigned some = __ballot_sync(0xffffffffu, there);
+#pragma unroll 8
+        for (int u = 0; u < n; ++u) {
+            const float fu = __shfl_sync(0xffffffffu, f, u);
+            if (!(some >> u & 1)) continue;                          // nothing was left there
+            const float *d = a.o + slot(i0 + u) * HD + lane * D;
+#pragma unroll
+            for (int j = 0; j < D; ++j) o[j] = fmaf(fu, d[j], o[j]);
+        }
+        if (n < 32) break;
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    QT *d = static_cast<QT *>(a.out) + ((size_t)(p.row0 + token) * a.H + head) * HD + lane * D;
+#pragma unroll
+    for (int j = 0; j < D; j += 2) {
+        if constexpr (sizeof(QT) == 2) *reinterpret_cast<uint32_t *>(d + j) = cvt_bf16x2(o[j] * inv, o[j + 1] * inv);
+        else *reinterpret_cast<float2 *>(d + j) = make_float2(o[j] * inv, o[j + 1] * inv);
+    }
+}
+
+}  // namespace attn
+}  // namespace knnssd

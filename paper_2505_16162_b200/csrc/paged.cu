@@ -4,6 +4,8 @@
 #include "host_common.cuh"
 #include "page_tables.cuh"
 #include "row_attention.cuh"
+#include "tensor_attention.cuh"
+#include "tensor_maps.cuh"
 
 #include <climits>
 #include <cmath>
@@ -26,7 +28,7 @@ template <typename K> bool allow_smem(K kernel, int bytes, bool (&done)[kMaxDevi
     return done[dev];
 }
 
-template <int HD, typename QT, typename KT, bool PAGED, int MB> knnssd_status launch_rows(rowattn::Args a, cudaStream_t s) {
+template <int HD, typename QT, typename KT, bool PAGED, int MB> knnssd_status launch_rows(attn::Args a, cudaStream_t s) {
     using Rg = rowattn::Ring<HD, KT>;
     static bool configured[kMaxDevices] = {};
     const auto kernel = rowattn::rows_kernel<HD, QT, KT, PAGED, MB>;
@@ -34,23 +36,67 @@ template <int HD, typename QT, typename KT, bool PAGED, int MB> knnssd_status la
     const int G = a.H / a.KV, most = 16 * MB;
     a.gs = (G + (G + most - 1) / most - 1) / ((G + most - 1) / most);
     a.subs = (G + a.gs - 1) / a.gs;
+    a.nvh = a.KV * a.subs;
     a.tb = most / a.gs;
     const int ctas = sm_count(), warps = ctas * Rg::WARPS;
     Scratch mem(s);
-    const size_t slots = (size_t)warps * rowattn::SLOTS * most;
+    const size_t slots = (size_t)warps * attn::SLOTS * most;
     if (!mem.get(&a.parts, (size_t)warps) || !mem.get(&a.ml, slots) || !mem.get(&a.o, slots * HD)) return KNNSSD_ERR_CUDA;
     launch_chained(kernel, dim3(ctas), dim3(Rg::WARPS * 32), Rg::SMEM, s, a);
-    launch_chained(rowattn::merge_kernel<HD, QT, MB>, dim3(warps - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
+    launch_chained(attn::merge_kernel<HD, QT, false, 16 * MB>, dim3(warps - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
     return launched();
 }
 
-template <int HD, bool PAGED> knnssd_status launch_types(const rowattn::Args &a, int dtype, int cache_dtype, int mb, cudaStream_t s) {
-    if (dtype == 0 && cache_dtype == 0) return launch_rows<HD, float, float, PAGED, 1>(a, s);
-    if constexpr (PAGED) {
-        if (dtype == 0) return launch_rows<HD, float, bf16_t, PAGED, 1>(a, s);
-        if (mb == 1) return launch_rows<HD, bf16_t, bf16_t, PAGED, 1>(a, s);
+// The word that the bounded waits of the tensor-core attention report to: the calls are asynchronous, nothing reads it but a debugger.
+__device__ int g_attention_err;
+int *attention_err_ptr() {
+    static int *addr[kMaxDevices] = {};
+    static std::mutex mu;
+    const int dev = current_device_slot();
+    std::lock_guard<std::mutex> lock(mu);
+    if (!addr[dev]) cudaGetSymbolAddress(reinterpret_cast<void **>(&addr[dev]), g_attention_err);
+    return addr[dev];
+}
+
+template <int HD, bool PAGED> knnssd_status launch_tensor(attn::Args a, cudaStream_t s) {
+    using L = tcattn::Lay<HD>;
+    static bool configured[kMaxDevices] = {};
+    const auto kernel = tcattn::tensor_kernel<HD, PAGED>;
+    a.err = attention_err_ptr();
+    if (!a.err || !allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
+    const int G = a.H / a.KV, most = tcattn::HALF_ROWS;
+    a.gs = (G + (G + most - 1) / most - 1) / ((G + most - 1) / most);
+    a.subs = (G + a.gs - 1) / a.gs;
+    a.nvh = a.KV * a.subs;
+    a.tb = most / a.gs;
+    a.extra = 128; a.least_run = 256;
+    CUtensorMap qm, km, vm;
+    const cuuint64_t qs[3] = {HD, (cuuint64_t)a.H, (cuuint64_t)a.R}, qst[2] = {HD * 2, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t qb[3] = {64, (cuuint32_t)a.gs, (cuuint32_t)a.tb};
+    bool made = bf16_map(&qm, a.q, 3, qs, qst, qb);
+    if (PAGED) {
+        const int page = 1 << a.page_shift;
+        const cuuint64_t ks[2] = {HD, (cuuint64_t)a.n_pages * a.KV * page}, kst[1] = {HD * 2};
+        const cuuint32_t kb[2] = {64, (cuuint32_t)(page < tcattn::KEYS ? page : tcattn::KEYS)};
+        made = made && bf16_map(&km, a.k, 2, ks, kst, kb) && bf16_map(&vm, a.v, 2, ks, kst, kb);
+    } else {
+        const cuuint64_t ks[3] = {HD, (cuuint64_t)a.KV, (cuuint64_t)a.R}, kst[2] = {HD * 2, (cuuint64_t)a.k_stride * 2}, vst[2] = {HD * 2, (cuuint64_t)a.v_stride * 2};
+        const cuuint32_t kb[3] = {64, 1, tcattn::KEYS};
+        made = made && bf16_map(&km, a.k, 3, ks, kst, kb) && bf16_map(&vm, a.v, 3, ks, vst, kb);
     }
-    return launch_rows<HD, bf16_t, bf16_t, PAGED, 2>(a, s);
+    if (!made) return KNNSSD_ERR_CUDA;
+    const int ctas = sm_count();
+    Scratch mem(s);
+    const size_t slots = (size_t)ctas * attn::SLOTS * tcattn::ROWS;
+    if (!mem.get(&a.parts, (size_t)ctas) || !mem.get(&a.ml, slots) || !mem.get(&a.o, slots * HD)) return KNNSSD_ERR_CUDA;
+    launch_chained(kernel, dim3(ctas), dim3(tcattn::NT), L::SMEM, s, a, qm, km, vm);
+    launch_chained(attn::merge_kernel<HD, bf16_t, true, tcattn::ROWS>, dim3(ctas - 1, tcattn::ROWS / 8), dim3(256), 0, s, a);
+    return launched();
+}
+
+template <int HD> knnssd_status launch_paged_rows(const attn::Args &a, int dtype, int cache_dtype, int mb, cudaStream_t s) {
+    if (dtype == 0) return cache_dtype == 0 ? launch_rows<HD, float, float, true, 1>(a, s) : launch_rows<HD, float, bf16_t, true, 1>(a, s);
+    return mb == 1 ? launch_rows<HD, bf16_t, bf16_t, true, 1>(a, s) : launch_rows<HD, bf16_t, bf16_t, true, 2>(a, s);
 }
 
 template <int HD> void launch_rotary(const pages::RotaryArgs &a, int dtype, int cache_dtype, cudaStream_t s) {
@@ -118,7 +164,7 @@ knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, lo
 knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, long long q_stride, int n_heads, int n_kv_heads, int head_dim, const void *k_pages_dev,
                                      const void *v_pages_dev, int cache_dtype, int page_size, int n_pages, const int *table_dev, int max_pages, const int *lens_dev,
                                      const int *row_start_dev, int n_requests, int max_fresh, float scale, void *out_dev, void *cuda_stream) {
-    if (n_rows < 0 || n_requests < 1 || max_fresh < 0 || !std::isfinite(scale)) return KNNSSD_ERR_INVALID_ARG;
+    if (n_rows < 0 || n_requests < 1 || max_fresh < 0 || !std::isfinite(scale) || scale < 0.f) return KNNSSD_ERR_INVALID_ARG;
     if (knnssd_status st = check_heads(dtype, cache_dtype, n_heads, n_kv_heads, head_dim); st != KNNSSD_OK) return st;
     if (knnssd_status st = check_pages(page_size, max_pages, n_pages); st != KNNSSD_OK) return st;
     if (n_rows > INT_MAX / 2) return KNNSSD_ERR_CAPACITY;
@@ -126,25 +172,33 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
     if (!q_dev || !k_pages_dev || !v_pages_dev || !table_dev || !lens_dev || !row_start_dev || !out_dev) return KNNSSD_ERR_INVALID_ARG;
     if (q_stride < (long long)n_heads * head_dim || q_stride % (dtype ? 8 : 4) != 0 || !aligned16(q_dev) || !aligned16(k_pages_dev) || !aligned16(v_pages_dev) || !aligned16(out_dev))
         return KNNSSD_ERR_SHAPE;
-    rowattn::Args a{};
+    attn::Args a{};
     a.q = q_dev; a.out = out_dev; a.q_stride = q_stride;
     a.k = k_pages_dev; a.v = v_pages_dev;
     a.table = table_dev; a.max_pages = max_pages; a.n_pages = n_pages;
     while ((1 << a.page_shift) < page_size) ++a.page_shift;
     a.lens = lens_dev; a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.most = INT_MAX; a.least_run = 64;
+    a.most = INT_MAX; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const int group = n_heads / n_kv_heads, mb = max_fresh > 0 && (long long)max_fresh * group <= 16 ? 1 : 2;
+    const int group = n_heads / n_kv_heads, most_rows = max_fresh > 0 && max_fresh < n_rows ? max_fresh : n_rows, mb = (long long)most_rows * group <= 16 ? 1 : 2;
+    if ((long long)n_pages * page_size * n_kv_heads > INT_MAX) return KNNSSD_ERR_CAPACITY;
+    const int few = group > 64 ? 1 : 64 / group;                     // what two passes of 32 rows over the pages do
     try {
-        return head_dim == 128 ? launch_types<128, true>(a, dtype, cache_dtype, mb, s) : launch_types<64, true>(a, dtype, cache_dtype, mb, s);
+        if (dtype == 1 && most_rows > few) {
+            a.most = few;
+            attn::Args b = a;
+            b.clear = 0;
+            if (const knnssd_status st = head_dim == 128 ? launch_tensor<128, true>(b, s) : launch_tensor<64, true>(b, s); st != KNNSSD_OK) return st;
+        }
+        return head_dim == 128 ? launch_paged_rows<128>(a, dtype, cache_dtype, mb, s) : launch_paged_rows<64>(a, dtype, cache_dtype, mb, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }
 }
 
 knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, const void *v_dev, int dtype, int n_rows, long long q_stride, long long k_stride,
                                       long long v_stride, int n_heads, int n_kv_heads, int head_dim, const int *row_start_dev, int n_requests, float scale, void *out_dev,
                                       void *cuda_stream) {
-    if (n_rows < 0 || n_requests < 1 || !std::isfinite(scale)) return KNNSSD_ERR_INVALID_ARG;
+    if (n_rows < 0 || n_requests < 1 || !std::isfinite(scale) || scale < 0.f) return KNNSSD_ERR_INVALID_ARG;
     if (knnssd_status st = check_heads(dtype, dtype, n_heads, n_kv_heads, head_dim); st != KNNSSD_OK) return st;
     if (n_rows > INT_MAX / 2) return KNNSSD_ERR_CAPACITY;
     if (n_rows == 0) return KNNSSD_OK;
@@ -154,15 +208,19 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
     if (q_stride < (long long)n_heads * head_dim || k_stride < kv_width || v_stride < kv_width || q_stride % per16 || k_stride % per16 || v_stride % per16 || !aligned16(q_dev) ||
         !aligned16(k_dev) || !aligned16(v_dev) || !aligned16(out_dev))
         return KNNSSD_ERR_SHAPE;
-    rowattn::Args a{};
+    attn::Args a{};
     a.q = q_dev; a.out = out_dev; a.q_stride = q_stride;
     a.k = k_dev; a.v = v_dev; a.k_stride = k_stride; a.v_stride = v_stride;
     a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.most = INT_MAX; a.least_run = 64;
+    a.most = INT_MAX; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
-        return head_dim == 128 ? launch_types<128, false>(a, dtype, dtype, 2, s) : launch_types<64, false>(a, dtype, dtype, 2, s);
+        if (dtype == 1) {
+            a.most = 0;
+            return head_dim == 128 ? launch_tensor<128, false>(a, s) : launch_tensor<64, false>(a, s);
+        }
+        return head_dim == 128 ? launch_rows<128, float, float, false, 1>(a, s) : launch_rows<64, float, float, false, 1>(a, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }
 }
 

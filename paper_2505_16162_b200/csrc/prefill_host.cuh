@@ -2,26 +2,15 @@
 #pragma once
 
 #include "prefill.cuh"
+#include "tensor_maps.cuh"
 
 #include <cuda_runtime.h>
 
 namespace knnssd {
 namespace prefill {
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's tensor-map encoder, looked up through the runtime (the library does not link against the driver).
-inline EncodeTiledFn encode_tiled_fn() {
-    static const EncodeTiledFn fn = [] {                 // once, and for all threads that come meanwhile
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
-        return found ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
-    }();
-    return fn;
-}
+using knnssd::encode_tiled_fn;
+using knnssd::EncodeTiledFn;
 
 // Map of a row-major bf16 matrix [rows][cols] (cols a multiple of 64) read in boxes of box_rows rows x 64 columns,
 // 128-byte swizzle; rows past the end read as zero.

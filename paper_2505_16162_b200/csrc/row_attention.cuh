@@ -16,137 +16,14 @@
 // term at most; in a sum of many it comes to less than the rounding of the result).
 #pragma once
 
-#include "device_common.cuh"
+#include "attention_items.cuh"
 
 namespace knnssd {
 namespace rowattn {
 
+using namespace attn;
+
 constexpr int TP = 16;                    // positions of a stage; pages and items begin at multiples of it
-constexpr int SLOTS = 2;                  // parts a warp may leave: of the item its run begins in, of the one it ends in
-
-struct Args {
-    const void *q;                        // [R][H][hd], rows q_stride elements apart
-    void *out;                            // [R][H][hd]
-    long long q_stride;
-    const void *k, *v;                    // pages [n_pages][KV][page][hd]; packed: [R][KV][hd], rows k_stride / v_stride elements apart
-    long long k_stride, v_stride;
-    const int *table;                     // [B][max_pages]
-    int max_pages, page_shift, n_pages;
-    const int *lens, *row_start;          // [B] (packed: nullptr, nothing held), [B + 1]
-    int B, R, H, KV;
-    float scale_log2;                     // scale log2 e: the softmax runs in powers of two
-    int gs, subs;                         // query heads of an item; items that share a K/V head's rows (heads of a group / gs)
-    int tb;                               // new rows of an item's block: tb gs <= 16 MB
-    int most;                             // requests of more new rows than this are another kernel's
-    int least_run;                        // positions a warp takes at least
-    // parts of items: what warp w knows of the item its run begins in, and its parts' (m, l) [w][SLOTS][16 MB] and o [w][SLOTS][16 MB][hd]
-    struct Part *parts;
-    float2 *ml;
-    float *o;
-};
-
-struct Request { int n, held, row0; long long cost; };
-// first: no run before this one begins within the item; [from, to): the run's positions of it; start: the item (-1: none)
-struct Part { long long start; int first, kv, from, to, row0, rows, vh, pad; };
-
-__device__ __forceinline__ Request request_of(const Args &a, int b) {
-    Request r;
-    const int r0 = min(max(a.row_start[b], 0), a.R), r1 = min(max(a.row_start[b + 1], 0), a.R);
-    r.n = max(r1 - r0, 0);
-    r.row0 = r0;
-    r.held = a.lens ? (int)min((long long)max(a.lens[b], 0), (long long)a.max_pages << a.page_shift) : 0;
-    if (r.n > a.most) r.n = 0;
-    const long long whole = r.n / a.tb, left = r.n % a.tb;
-    r.cost = (whole * r.held + a.tb * (whole * (whole + 1) / 2) + (left ? r.held + r.n : 0)) * a.KV * a.subs;
-    return r;
-}
-
-// An item and where it begins among all items' positions.
-struct Item {
-    Request r;
-    int b, rb, vh, kv;                    // kv: positions that the block's last row sees
-    long long start;
-    __device__ __forceinline__ void see(const Args &a) { kv = r.held + min(a.tb * (rb + 1), r.n); }
-    __device__ __forceinline__ int tokens(const Args &a) const { return min(a.tb, r.n - rb * a.tb); }
-    // the item behind this one; false when there is none
-    __device__ __forceinline__ bool next(const Args &a) {
-        start += kv;
-        if (++vh < a.KV * a.subs) return true;
-        vh = 0;
-        if (++rb * a.tb < r.n) { see(a); return true; }
-        rb = 0;
-        while (++b < a.B) {
-            r = request_of(a, b);
-            if (r.cost > 0) { see(a); return true; }
-        }
-        return false;
-    }
-};
-
-// A block's view of the requests: the costs of NCH runs of them, summed.
-template <int NCH> struct Costs {
-    long long pfx[NCH + 1];
-    long long warp_sum[NCH / 32];
-};
-
-// All threads of the block (NCH of them).
-template <int NCH> __device__ __forceinline__ void sum_costs(const Args &a, Costs<NCH> &c) {
-    const int tid = threadIdx.x, per = (a.B + NCH - 1) / NCH, lane = tid & 31;
-    long long v = 0;
-    for (int b = tid * per; b < min((tid + 1) * per, a.B); ++b) v += request_of(a, b).cost;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += u;
-    }
-    if (lane == 31) c.warp_sum[tid >> 5] = v;
-    __syncthreads();
-    for (int w = 0; w < tid >> 5; ++w) v += c.warp_sum[w];
-    c.pfx[tid + 1] = v;
-    if (tid == 0) c.pfx[0] = 0;
-    __syncthreads();
-}
-
-// The item that position x of all items' lies in; x < the sum.
-template <int NCH> __device__ __forceinline__ Item item_at(const Args &a, const Costs<NCH> &c, long long x) {
-    int lo = 0, hi = NCH - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (c.pfx[mid + 1] > x) hi = mid; else lo = mid + 1;
-    }
-    Item it;
-    it.start = c.pfx[lo];
-    it.b = lo * ((a.B + NCH - 1) / NCH);
-    for (;; ++it.b) {
-        it.r = request_of(a, it.b);
-        if (x < it.start + it.r.cost) break;
-        it.start += it.r.cost;
-    }
-    // block rb begins at VH (rb held + tb rb (rb + 1) / 2)
-    const long long VH = (long long)a.KV * a.subs, at = x - it.start;
-    auto before = [&](long long rb) { return VH * (rb * it.r.held + a.tb * (rb * (rb + 1) / 2)); };
-    int r0 = 0, r1 = (it.r.n + a.tb - 1) / a.tb - 1;
-    while (r0 < r1) {
-        const int mid = (r0 + r1) >> 1;
-        if (before(mid + 1) > at) r1 = mid; else r0 = mid + 1;
-    }
-    it.rb = r0;
-    it.see(a);
-    it.vh = (int)((at - before(r0)) / it.kv);
-    it.start += before(r0) + (long long)it.vh * it.kv;
-    return it;
-}
-
-__device__ __forceinline__ long long up16(long long x) { return (x + TP - 1) & ~(long long)(TP - 1); }
-// The run of warp w of W, and the part [from, to) of an item that lies in it: runs are cut at the next multiple of TP of the item.
-__device__ __forceinline__ long long run_start(long long total, int w, int W) { return total / W * w + total % W * w / W; }
-__device__ __forceinline__ int cut(const Item &it, long long x) {
-    return (int)(x <= it.start ? 0 : min(up16(x - it.start), (long long)it.kv));
-}
-
-__device__ __forceinline__ int warps_of(const Args &a, long long total, int most) {
-    return (int)max(1ll, min((long long)most, total / a.least_run));
-}
 
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -164,11 +41,6 @@ __device__ __forceinline__ uint4 lds16(uint32_t p) {
 }
 __device__ __forceinline__ void ldsm4t(uint32_t p, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(p));
-}
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 // (v0, v1) as N bf16 pairs whose sums they are (N = 1: rounded to nearest).
 template <int N> __device__ __forceinline__ void terms_of(float v0, float v1, uint32_t (&t)[N]) {
@@ -200,14 +72,10 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
     __shared__ int hole_of[Rg::WARPS][Rg::STAGES];
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    sum_costs<NT>(a, costs);
-    {   // rows behind the last request's are nobody's: zeros
-        const int used = min(max(a.row_start[a.B], 0), a.R);
-        QT *o = static_cast<QT *>(a.out);
-        for (long long i = (long long)used * a.H * HD + (long long)blockIdx.x * NT + threadIdx.x; i < (long long)a.R * a.H * HD; i += (long long)gridDim.x * NT) o[i] = QT(0);
-    }
+    sum_costs<false>(a, costs);
+    if (a.clear) clear_tail<QT>(a, HD, blockIdx.x * NT + threadIdx.x, gridDim.x * NT);
     const long long total = costs.pfx[NT];
-    const int W = warps_of(a, total, gridDim.x * Rg::WARPS);
+    const int W = workers_of(a, total, gridDim.x * Rg::WARPS);
     // neighbouring runs go to different SMs: a short launch spreads over the chip
     const int w = warp * gridDim.x + blockIdx.x;
     const long long x0 = w < W ? run_start(total, w, W) : 0, x1 = w < W ? run_start(total, w + 1, W) : 0;
@@ -215,26 +83,19 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
         if (lane == 0) { a.parts[w].first = 0; a.parts[w].start = -1; }
         return;
     }
-    Item in = item_at<NT>(a, costs, x0);                             // the item whose positions are being fetched
-    Item it = in;                                                    // the item at work
-    if (lane == 0) {
-        Part p;
-        p.start = it.start;
-        p.from = cut(it, x0); p.to = cut(it, x1); p.kv = it.kv;
-        p.first = p.from > 0 && p.from < it.kv && run_start(total, w - 1, W) <= it.start;
-        p.row0 = it.r.row0 + it.rb * a.tb; p.rows = it.tokens(a); p.vh = it.vh; p.pad = 0;
-        a.parts[w] = p;
-    }
+    Item<false> in = item_at<false>(a, costs, x0);                   // the item whose positions are being fetched
+    Item<false> it = in;                                             // the item at work
+    if (lane == 0) note_part<TP>(a, it, w, W, total, x0, x1);
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * Rg::STAGES * Rg::STAGE;
 
     // ---- fetching -------------------------------------------------------------------------------------------------
-    int at = cut(in, x0), until = cut(in, x1);
+    int at = cut<TP>(in, x0), until = cut<TP>(in, x1);
     bool more = true;
     int pid = 0;                                                     // the page of the next 16 positions
     auto settle = [&]() {                                            // on to the next positions that are this warp's
         while (more && at >= until) {
             more = in.next(a) && in.start < x1;
-            if (more) { at = 0; until = cut(in, x1); }
+            if (more) { at = 0; until = cut<TP>(in, x1); }
         }
         if (PAGED && more) {
             const int idx = at >> a.page_shift;
@@ -279,9 +140,9 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
     int stage = 0;
     bool any = true;
     while (any) {
-        const int from = cut(it, x0), to = cut(it, x1);
+        const int from = cut<TP>(it, x0), to = cut<TP>(it, x1);
         if (from < to) {
-            const int row0 = it.r.row0 + it.rb * a.tb, tokens = it.tokens(a), kvh = it.vh / a.subs, G = a.H / a.KV;
+            const int row0 = it.r.row0 + it.rb * it.r.tb, tokens = it.tokens(), kvh = it.vh / a.subs, G = a.H / a.KV;
             const int h0 = kvh * G + (it.vh % a.subs) * a.gs, heads = min(a.gs, (kvh + 1) * G - h0), live = tokens * heads;
             const int seen0 = it.kv - tokens;                        // position of the block's first row
             // dimension pair h of k-step s that lane t multiplies: any order serves a dot product, this one makes 16-byte reads of K
@@ -518,63 +379,6 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                 }
         }
         any = it.next(a) && it.start < x1;
-    }
-}
-
-// Items in parts.  Block (w, j) does eight rows, j 8 .., of the item that warp w's run is the first to begin within: the part of warp w - 1
-// and those behind it until the item's end, in their order.  A warp per row: its lanes share the parts' (m, l) out, then hd / 32
-// dimensions each.
-template <int HD, typename QT, int MB>
-__global__ void __launch_bounds__(256) merge_kernel(const Args a) {
-    chain_wait();
-    const int w = blockIdx.x + 1, lane = threadIdx.x & 31;
-    const Part p = a.parts[w];
-    if (!p.first) return;
-    const int G = a.H / a.KV, kvh = p.vh / a.subs, h0 = kvh * G + (p.vh % a.subs) * a.gs, heads = min(a.gs, (kvh + 1) * G - h0);
-    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
-    if (r >= p.rows * heads) return;
-    // part i: of run w - 1 + i, as long as the runs begin in this item
-    auto slot = [&](int i) { return ((size_t)(w - 1 + i) * SLOTS + (i == 0 ? 1 : 0)) * (16 * MB) + r; };
-    const int most = gridDim.x + 2 - w;
-    constexpr int D = HD / 32;
-    float o[D], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < D; ++i) o[i] = 0.f;
-    for (int i0 = 0;; i0 += 32) {
-        const int i = i0 + lane;
-        bool mine = i < most, there = mine;                          // there: not cut away
-        if (mine && i > 0) {
-            const Part *q = a.parts + w - 1 + i;
-            mine = q->start == p.start;
-            there = mine && q->from < q->to;
-        }
-        const unsigned all = __ballot_sync(0xffffffffu, mine);
-        const int n = all == 0xffffffffu ? 32 : __ffs(~all) - 1;      // lanes up to the first that is not of the item
-        there = there && lane < n;
-        const float2 v = there ? a.ml[slot(i)] : make_float2(-INFINITY, 0.f);
-        const float mn = fmaxf(m, warp_max(v.x)), base = mn == -INFINITY ? 0.f : mn;
-        const float f = exp2_approx(v.x - base), old = exp2_approx(m - base);
-        l = l * old + warp_sum(v.y * f);
-#pragma unroll
-        for (int j = 0; j < D; ++j) o[j] *= old;
-        m = mn;
-        const unsigned some = __ballot_sync(0xffffffffu, there);
-#pragma unroll 8
-        for (int u = 0; u < n; ++u) {
-            const float fu = __shfl_sync(0xffffffffu, f, u);
-            if (!(some >> u & 1)) continue;                          // nothing was left there
-            const float *d = a.o + slot(i0 + u) * HD + lane * D;
-#pragma unroll
-            for (int j = 0; j < D; ++j) o[j] = fmaf(fu, d[j], o[j]);
-        }
-        if (n < 32) break;
-    }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    QT *d = static_cast<QT *>(a.out) + ((size_t)(p.row0 + r / heads) * a.H + h0 + r % heads) * HD + lane * D;
-#pragma unroll
-    for (int j = 0; j < D; j += 2) {
-        if constexpr (sizeof(QT) == 2) *reinterpret_cast<uint32_t *>(d + j) = cvt_bf16x2(o[j] * inv, o[j + 1] * inv);
-        else *reinterpret_cast<float2 *>(d + j) = make_float2(o[j] * inv, o[j + 1] * inv);
     }
 }
 
