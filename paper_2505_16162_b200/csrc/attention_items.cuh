@@ -222,8 +222,19 @@ __global__ void __launch_bounds__(256) merge_kernel(const Args a) {
 #pragma unroll 8
         for (int u = 0; u < n; ++u) {
             const float fu = __shfl_sync(0xffffffffu, f, u);
-            if (!(some >> u & 1)) continue;                          // nothing was left there
-            const float *d = a.o + slot(i0 + u) * HD + lane * D;
+            float d[D];
+#pragma unroll
+            for (int j = 0; j < D; ++j) d[j] = 0.f;
+            if (some >> u & 1) {
+                const float *src = a.o + slot(i0 + u) * HD + lane * D;
+                if constexpr (D == 4) {
+                    const float4 v4 = *reinterpret_cast<const float4 *>(src);
+                    d[0] = v4.x; d[1] = v4.y; d[2] = v4.z; d[3] = v4.w;
+                } else {
+                    const float2 v2 = *reinterpret_cast<const float2 *>(src);
+                    d[0] = v2.x; d[1] = v2.y;
+                }
+            }
 #pragma unroll
             for (int j = 0; j < D; ++j) o[j] = fmaf(fu, d[j], o[j]);
         }

@@ -179,7 +179,7 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
     while ((1 << a.page_shift) < page_size) ++a.page_shift;
     a.lens = lens_dev; a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.most = INT_MAX; a.least_run = 64; a.clear = 1;
+    a.most = INT_MAX; a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     const int group = n_heads / n_kv_heads, most_rows = max_fresh > 0 && max_fresh < n_rows ? max_fresh : n_rows, mb = (long long)most_rows * group <= 16 ? 1 : 2;
     if ((long long)n_pages * page_size * n_kv_heads > INT_MAX) return KNNSSD_ERR_CAPACITY;
@@ -213,7 +213,7 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
     a.k = k_dev; a.v = v_dev; a.k_stride = k_stride; a.v_stride = v_stride;
     a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.most = INT_MAX; a.least_run = 64; a.clear = 1;
+    a.most = INT_MAX; a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if (dtype == 1) {

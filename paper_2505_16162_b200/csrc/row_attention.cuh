@@ -26,9 +26,9 @@ using namespace attn;
 constexpr int TP = 16;                    // positions of a stage; pages and items begin at multiples of it
 
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
     const int n = there ? 16 : 0;                                    // 0: the 16 bytes become zeros
@@ -188,17 +188,22 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                 const bool hole = PAGED && hole_of[warp][stage] != 0;
                 const uint32_t kb = ring + stage * Rg::STAGE, vb = kb + TP * Rg::ROW;
                 fetch();                                             // into the stage that the positions before have left
-                float s[MB][2][4];
+                // The tensor cores add to a sum by truncation.  Where fp32 is answered a sum gets few such additions: the small terms have a sum of
+                // their own, and the 16 positions' share of o is added to it by an ordinary addition.
+                constexpr int NS = NQ == 1 ? 2 : 3;                  // sums of the scores, all independent chains
+                float sp[MB][2][NS][4];
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                     for (int n = 0; n < 2; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[mb][n][i] = 0.f;
+                        for (int u = 0; u < NS; ++u)
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                            for (int i = 0; i < 4; ++i) sp[mb][n][u][i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < HD / 32; ++c) {
+                for (int c = 0; c < HD / 32; ++c)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
                         const int pos = 8 * n + g;
                         if constexpr (NK == 1) {
                             const uint4 w = lds16(kb + pos * Rg::ROW + Rg::kswz(pos, 4 * c + t) * 16);
@@ -206,8 +211,8 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                                 for (int i = NQ - 1; i >= 0; --i) {
-                                    mma(s[mb][n], qf[mb][2 * c][i], w.x, w.y);
-                                    mma(s[mb][n], qf[mb][2 * c + 1][i], w.z, w.w);
+                                    mma(sp[mb][n][i ? 2 : 0], qf[mb][2 * c][i], w.x, w.y);
+                                    mma(sp[mb][n][i ? 2 : 1], qf[mb][2 * c + 1][i], w.z, w.w);
                                 }
                         } else {
 #pragma unroll
@@ -221,10 +226,17 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
 #pragma unroll
                                     for (int i = NQ - 1; i >= 0; --i)
 #pragma unroll
-                                        for (int j = NK - 1 - i; j >= 0; --j) mma(s[mb][n], qf[mb][2 * c + e][i], b0[j], b1[j]);
+                                        for (int j = NK - 1 - i; j >= 0; --j) mma(sp[mb][n][i + j ? 2 : e], qf[mb][2 * c + e][i], b0[j], b1[j]);
                             }
                         }
                     }
+                float s[MB][2][4];
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[mb][n][i] = sp[mb][n][0][i] + sp[mb][n][1][i] + (NS == 3 ? sp[mb][n][NS - 1][i] : 0.f);
                 const bool ragged = hole || p + TP - 1 > seen0;      // some row does not see all of these positions
                 uint32_t pf[MB][NQ][4];
 #pragma unroll
@@ -263,11 +275,19 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                 bool odd = false;
                 auto products = [&](int n, const uint32_t (&b0)[NK], const uint32_t (&b1)[NK]) {
 #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb)
+                    for (int mb = 0; mb < MB; ++mb) {
+                        if constexpr (NQ == 1) {
+                            mma(o[mb][n], pf[mb][0], b0[0], b1[0]);
+                        } else {
+                            float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int i = NQ - 1; i >= 0; --i)
+                            for (int i = NQ - 1; i >= 0; --i)
 #pragma unroll
-                            for (int j = NK == 1 ? 0 : NK - 1 - i; j >= 0; --j) mma(o[mb][n], pf[mb][i], b0[j], b1[j]);
+                                for (int j = NK == 1 ? 0 : NK - 1 - i; j >= 0; --j) mma(d, pf[mb][i], b0[j], b1[j]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[mb][n][i] += d[i];
+                        }
+                    }
                 };
                 // the same, position by position, into the rows that see it
                 auto products_apart = [&](int n, const uint32_t (&b0)[NK], const uint32_t (&b1)[NK]) {
