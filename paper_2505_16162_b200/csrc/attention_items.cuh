@@ -27,7 +27,6 @@ struct Args {
     float scale_log2;                     // scale log2 e: the softmax runs in powers of two
     int gs, subs, nvh;                    // query heads of an item; items that share a K/V head's rows (heads of a group / gs); KV subs
     int tb;                               // new rows of a block (of half a block, where blocks have two halves)
-    int most;                             // requests of up to this many new rows are the rows kernel's, the others the tensor kernel's
     int extra;                            // positions that an item's beginning and end cost
     int least_run;                        // positions a worker takes at least
     int clear;                            // rows that no request has are this launch's to clear
@@ -51,7 +50,6 @@ template <bool HALVES> __device__ __forceinline__ Request request_of(const Args 
     r.n = max(r1 - r0, 0);
     r.row0 = r0;
     r.held = a.lens ? (int)min((long long)max(a.lens[b], 0), (long long)a.max_pages << a.page_shift) : 0;
-    if (HALVES ? r.n <= a.most : r.n > a.most) r.n = 0;
     r.tb = HALVES && r.n > a.tb ? 2 * a.tb : a.tb;
     r.nvh = HALVES && r.n <= a.tb ? (a.nvh + 1) / 2 : a.nvh;
     const long long whole = r.n / r.tb, left = r.n % r.tb, each = (long long)r.held + a.extra;

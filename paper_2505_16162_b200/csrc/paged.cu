@@ -94,9 +94,8 @@ template <int HD, bool PAGED> knnssd_status launch_tensor(attn::Args a, cudaStre
     return launched();
 }
 
-template <int HD> knnssd_status launch_paged_rows(const attn::Args &a, int dtype, int cache_dtype, int mb, cudaStream_t s) {
-    if (dtype == 0) return cache_dtype == 0 ? launch_rows<HD, float, float, true, 1>(a, s) : launch_rows<HD, float, bf16_t, true, 1>(a, s);
-    return mb == 1 ? launch_rows<HD, bf16_t, bf16_t, true, 1>(a, s) : launch_rows<HD, bf16_t, bf16_t, true, 2>(a, s);
+template <int HD> knnssd_status launch_paged_rows(const attn::Args &a, int cache_dtype, cudaStream_t s) {
+    return cache_dtype == 0 ? launch_rows<HD, float, float, true, 1>(a, s) : launch_rows<HD, float, bf16_t, true, 1>(a, s);
 }
 
 template <int HD> void launch_rotary(const pages::RotaryArgs &a, int dtype, int cache_dtype, cudaStream_t s) {
@@ -179,19 +178,12 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
     while ((1 << a.page_shift) < page_size) ++a.page_shift;
     a.lens = lens_dev; a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.most = INT_MAX; a.extra = 64; a.least_run = 64; a.clear = 1;
+    a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const int group = n_heads / n_kv_heads, most_rows = max_fresh > 0 && max_fresh < n_rows ? max_fresh : n_rows, mb = (long long)most_rows * group <= 16 ? 1 : 2;
     if ((long long)n_pages * page_size * n_kv_heads > INT_MAX) return KNNSSD_ERR_CAPACITY;
-    const int few = group > 64 ? 1 : 64 / group;                     // what two passes of 32 rows over the pages do
     try {
-        if (dtype == 1 && most_rows > few) {
-            a.most = few;
-            attn::Args b = a;
-            b.clear = 0;
-            if (const knnssd_status st = head_dim == 128 ? launch_tensor<128, true>(b, s) : launch_tensor<64, true>(b, s); st != KNNSSD_OK) return st;
-        }
-        return head_dim == 128 ? launch_paged_rows<128>(a, dtype, cache_dtype, mb, s) : launch_paged_rows<64>(a, dtype, cache_dtype, mb, s);
+        if (dtype == 1) return head_dim == 128 ? launch_tensor<128, true>(a, s) : launch_tensor<64, true>(a, s);
+        return head_dim == 128 ? launch_paged_rows<128>(a, cache_dtype, s) : launch_paged_rows<64>(a, cache_dtype, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }
 }
 
@@ -213,11 +205,10 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
     a.k = k_dev; a.v = v_dev; a.k_stride = k_stride; a.v_stride = v_stride;
     a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.most = INT_MAX; a.extra = 64; a.least_run = 64; a.clear = 1;
+    a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if (dtype == 1) {
-            a.most = 0;
             return head_dim == 128 ? launch_tensor<128, false>(a, s) : launch_tensor<64, false>(a, s);
         }
         return head_dim == 128 ? launch_rows<128, float, float, false, 1>(a, s) : launch_rows<64, float, float, false, 1>(a, s);

@@ -425,11 +425,18 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                 place_of<true, ROWS>(a, job.tokens, it.vh, job.paired, r, token, head);
                 const int last = token >= 0 ? job.seen0 + token : -1, first_last = job.seen0 + (job.paired ? 0 : h * a.tb);
                 const size_t row = (size_t)(it.r.row0 + it.rb * it.r.tb + (token < 0 ? 0 : token)) * a.H + head;
+                const bool live = __any_sync(0xffffffffu, token >= 0);
                 float m = -INFINITY, l = 0.f;
                 for (int s = 0; s < job.n[h] && ok; ++s) {
                     const int k0 = (job.j0 + s) * KEYS;
                     ok = bar_wait(s_full + 8 * h, s_uses++ & 1, &quit, a.err, 208);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    if (!live) {                                     // none of the warp's rows is anyone's: what is in P there stays there
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(p_full + 8 * h);
+                        ++o_uses;
+                        continue;
+                    }
                     fence_after();
                     uint32_t x[4][32];
 #pragma unroll
@@ -502,7 +509,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                     fence_after();
                 }
-                if (job.n[h] || (job.from < job.to && !whole)) {
+                if (live && (job.n[h] || (job.from < job.to && !whole))) {
                     const float f = whole ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
                     const size_t slot = ((size_t)w * SLOTS + (job.from > 0 ? 0 : 1)) * ROWS + r;
                     bool odd = false;
