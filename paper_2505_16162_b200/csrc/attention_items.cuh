@@ -27,6 +27,7 @@ struct Args {
     float scale_log2;                     // scale log2 e: the softmax runs in powers of two
     int gs, subs, nvh;                    // query heads of an item; items that share a K/V head's rows (heads of a group / gs); KV subs
     int tb;                               // new rows of a block (of half a block, where blocks have two halves)
+    int pair_most;                        // positions up to which the halves of a block take two heads of a request with few rows
     int extra;                            // positions that an item's beginning and end cost
     int least_run;                        // positions a worker takes at least
     int clear;                            // rows that no request has are this launch's to clear
@@ -41,8 +42,8 @@ struct Args {
 struct Part { long long start; int first, kv, from, to, row0, rows, vh, paired; };
 
 // A request's new rows n, what it held before, the block's rows tb and the items nvh per block.  HALVES: a block has two halves of a.tb rows each;
-// where a request has no more than one of them, the halves take two heads instead.
-struct Request { int n, held, row0, tb, nvh; long long cost; };
+// where a request has no more rows than one of them and few positions, the halves take two heads instead (paired).
+struct Request { int n, held, row0, tb, nvh; bool paired; long long cost; };
 
 template <bool HALVES> __device__ __forceinline__ Request request_of(const Args &a, int b) {
     Request r;
@@ -50,8 +51,9 @@ template <bool HALVES> __device__ __forceinline__ Request request_of(const Args 
     r.n = max(r1 - r0, 0);
     r.row0 = r0;
     r.held = a.lens ? (int)min((long long)max(a.lens[b], 0), (long long)a.max_pages << a.page_shift) : 0;
-    r.tb = HALVES && r.n > a.tb ? 2 * a.tb : a.tb;
-    r.nvh = HALVES && r.n <= a.tb ? (a.nvh + 1) / 2 : a.nvh;
+    r.paired = HALVES && r.n <= a.tb && r.held + r.n <= a.pair_most;
+    r.tb = HALVES && !r.paired ? 2 * a.tb : a.tb;
+    r.nvh = r.paired ? (a.nvh + 1) / 2 : a.nvh;
     const long long whole = r.n / r.tb, left = r.n % r.tb, each = (long long)r.held + a.extra;
     r.cost = (whole * each + r.tb * (whole * (whole + 1) / 2) + (left ? each + r.n : 0)) * r.nvh;
     return r;
@@ -64,8 +66,6 @@ template <bool HALVES> struct Item {
     long long start;
     __device__ __forceinline__ void see() { kv = r.held + min(r.tb * (rb + 1), r.n); }
     __device__ __forceinline__ int tokens() const { return min(r.tb, r.n - rb * r.tb); }
-    __device__ __forceinline__ bool paired() const { return HALVES && r.n <= r.tb && r.tb == tb_half; }
-    int tb_half;
     // the item behind this one; false when there is none
     __device__ __forceinline__ bool next(const Args &a) {
         start += kv + a.extra;
@@ -116,7 +116,6 @@ template <bool HALVES, int N> __device__ __forceinline__ Item<HALVES> item_at(co
         if (c.pfx[mid + 1] > x) hi = mid; else lo = mid + 1;
     }
     Item<HALVES> it;
-    it.tb_half = a.tb;
     it.start = c.pfx[lo];
     it.b = lo * ((a.B + N - 1) / N);
     for (;; ++it.b) {
@@ -152,7 +151,7 @@ template <int TP, bool HALVES> __device__ __forceinline__ void note_part(const A
     p.start = it.start;
     p.from = cut<TP>(it, x0); p.to = cut<TP>(it, x1); p.kv = it.kv;
     p.first = p.from > 0 && p.from < it.kv && run_start(total, w - 1, W) <= it.start;
-    p.row0 = it.r.row0 + it.rb * it.r.tb; p.rows = it.tokens(); p.vh = it.vh; p.paired = it.paired();
+    p.row0 = it.r.row0 + it.rb * it.r.tb; p.rows = it.tokens(); p.vh = it.vh; p.paired = it.r.paired;
     a.parts[w] = p;
 }
 

@@ -69,7 +69,7 @@ template <int HD, bool PAGED> knnssd_status launch_tensor(attn::Args a, cudaStre
     a.subs = (G + a.gs - 1) / a.gs;
     a.nvh = a.KV * a.subs;
     a.tb = most / a.gs;
-    a.extra = 128; a.least_run = 256;
+    a.extra = 384; a.least_run = 512; a.pair_most = 1024;
     CUtensorMap qm, km, vm;
     const cuuint64_t qs[3] = {HD, (cuuint64_t)a.H, (cuuint64_t)a.R}, qst[2] = {HD * 2, (cuuint64_t)a.q_stride * 2};
     const cuuint32_t qb[3] = {64, (cuuint32_t)a.gs, (cuuint32_t)a.tb};

@@ -1,17 +1,19 @@
 // Attention of many new rows on the 5th-generation tensor cores: bf16 queries over pages or over packed prompts.
 //
 // The mathematics is the rows kernel's.  A block of a launch (one per SM) takes two halves of 128 rows (query heads that share a K/V head times
-// new rows) through the positions 128 at a time:
+// new rows) through the positions, in tiles of 128 and steps of 64:
 //
-//   warp 8       brings q, K and V in by TMA (128-byte swizzle), a ring of 128-position tiles ahead of the products
-//   warp 9       issues the products: S = q K^T into tensor memory, O += P V with P read from tensor memory and V as the
+//   warp 8       brings q, K and V in by TMA (128-byte swizzle), a ring of tiles ahead of the products
+//   warps 9, 10  issue the products of a half each: S = q K^T into tensor memory, O += P V with P read from tensor memory and V as the
 //                transposed operand straight from its row-major tile
 //   warps 0 - 3  the softmax of the first half, a row per thread: scores out of tensor memory, exponentials, P back as bf16 over them
 //   warps 4 - 7  the same for the second half
 //
-// While one half's exponentials are formed the tensor cores do the other half's products, in the order S0 S1 | PV0 S0' PV1 S1' | ..  O stays in tensor
-// memory; it is multiplied only when a row's maximum has grown by more than 2^8 since the reference its exponentials are taken against
-// (their sums stay far inside fp32, and bf16 rounds relatively), which hardly ever happens after the first positions.
+// Each half has two score buffers of 64 columns: while the softmax works on one step the scores of the next are formed in the other, so
+// that neither the softmax nor the tensor cores wait out the other's latency (with one buffer of 128 columns a step of 128 positions
+// took softmax + products, 3900 .. 4700 clocks, one half's softmax under the other half's products).  O stays in tensor memory; it is multiplied
+// only when a row's maximum has grown by more than 2^8 since the reference its exponentials are taken against (their sums stay far inside
+// fp32, and bf16 rounds relatively), which hardly ever happens after the first positions.
 // Both halves share the K/V tiles; where a request has no more rows than one half, the halves are two K/V heads with tiles of their own.
 //
 // Every wait is bounded; one that gives up sets the error word and all warps leave, after their copies have landed.
@@ -26,14 +28,14 @@ namespace tcattn {
 
 using namespace attn;
 
-constexpr int KEYS = 128, HALF_ROWS = 128, ROWS = 256;
-constexpr int SOFT_WARPS = 8, NT = (SOFT_WARPS + 4) * 32, LOAD_WARP = 8, MMA_WARP = 9;
-constexpr int SOFT_REGS = 216, OTHER_REGS = 72;     // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the block is launched with
+constexpr int KEYS = 128, SUB = 64, HALF_ROWS = 128, ROWS = 256;      // positions of a tile, and of a step of the softmax
+constexpr int SOFT_WARPS = 8, NT = (SOFT_WARPS + 3) * 32, LOAD_WARP = 8, MMA_WARP = 9;
 constexpr int NCOST = 128;
 constexpr int BAND = KEYS * 128;          // bytes of 64 dimensions of a tile: rows of 128 bytes, swizzled
 constexpr int INFO = 16;                  // steps whose page masks are kept
 constexpr unsigned WAIT_LIMIT = 1000000u;
 constexpr float GROWTH = 8.f;
+constexpr int CUBIC = 1, CUBIC_OF = 4;     // one pair in four takes its powers of two from the multiply-add units
 constexpr int TMEM_COLS = 512, O_COL = 256;
 
 template <int HD> struct Lay {
@@ -65,10 +67,9 @@ __device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity, volatile i
     }
     return true;
 }
-__device__ __forceinline__ uint32_t elect() {
-    uint32_t one;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-    return one;
+// The same for a warp as a whole: all lanes go on, or none.
+__device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int *quit, int *err, int code) {
+    return __all_sync(0xffffffffu, bar_wait(b, parity, quit, err, code));
 }
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y)
@@ -82,25 +83,40 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int
 // Shared-memory operand descriptors, 128-byte swizzle: address / 16 in bits 0 .. 13, leading offset / 16 in 16 .. 29, stride offset / 16 in
 // 32 .. 45, version 1 in 46 .. 47, swizzle mode 2 in 61 .. 63.  Rows are 128 bytes, eight of them (1024 bytes) the stride.  Read along
 // the dimensions (q, K): the leading offset plays no part.  Read along the positions (V, the transposed operand): it leads to the next 64 dimensions.
-__device__ __forceinline__ uint64_t desc_of(uint32_t addr) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(BAND >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
+// The constant upper half, and the lower half.
+constexpr uint32_t DESC_UPPER = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_of(uint32_t addr) { return (addr >> 4) | ((uint32_t)(BAND >> 4) << 16); }
 // fp32 sums, bf16 operands, M = 128, N columns; transposed: the second operand is read along its rows.
 __host__ __device__ constexpr uint32_t idesc_of(int n, bool transposed) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (transposed ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add, uint32_t one) {
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
-                 "r"(idesc), "r"(add), "r"(one)
+// A row of products as one piece of code, so that their operands differ from one another by constants; one thread of the warp issues them.
+#define KNNSSD_SS(K) "add.u32 x, %1, " K ";\n\tadd.u32 y, %2, " K ";\n\tmov.b64 da, {x, %5};\n\tmov.b64 db, {y, %5};\n\t"
+#define KNNSSD_SS_FIRST "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, 0;\n\t"
+#define KNNSSD_SS_NEXT(K) KNNSSD_SS(K) "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, 1;\n\t"
+// S (128 x 64) = q k^T over HD dimensions: steps of 16 are 32 bytes apart, the second 64 dimensions a band further; then bar is told.
+template <int HD> __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t q, uint32_t k, uint32_t idesc, uint32_t bar) {
+    if constexpr (HD == 128)
+        asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 da, db;\n\t.reg .b32 x, y;\n\telect.sync _|q, 0xffffffff;\n\t" KNNSSD_SS_FIRST KNNSSD_SS_NEXT("2") KNNSSD_SS_NEXT("4")
+                     KNNSSD_SS_NEXT("6") KNNSSD_SS_NEXT("1024") KNNSSD_SS_NEXT("1026") KNNSSD_SS_NEXT("1028") KNNSSD_SS_NEXT("1030")
+                     "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t}" ::"r"(d), "r"(q), "r"(k), "r"(idesc), "r"(bar), "r"(DESC_UPPER)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 da, db;\n\t.reg .b32 x, y;\n\telect.sync _|q, 0xffffffff;\n\t" KNNSSD_SS_FIRST KNNSSD_SS_NEXT("2") KNNSSD_SS_NEXT("4")
+                     KNNSSD_SS_NEXT("6") "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t}" ::"r"(d), "r"(q), "r"(k), "r"(idesc), "r"(bar),
+                     "r"(DESC_UPPER)
+                     : "memory");
+}
+#define KNNSSD_TS_NEXT(A, B) "add.u32 x, %1, " A ";\n\tadd.u32 y, %2, " B ";\n\tmov.b64 db, {y, %5};\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %3, 1;\n\t"
+// O (128 x HD) += P V over 64 positions: P 8 columns a step of 16, V 2048 bytes.  add 0: the first product begins the sum.  Then bar is told.
+__device__ __forceinline__ void mma_values(uint32_t d, uint32_t p, uint32_t v, uint32_t idesc, uint32_t add, uint32_t bar) {
+    asm volatile("{\n\t.reg .pred q, a;\n\t.reg .b64 db;\n\t.reg .b32 x, y;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 a, %4, 0;\n\tmov.b64 db, {%2, %5};\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, a;\n\t" KNNSSD_TS_NEXT("8", "128") KNNSSD_TS_NEXT("16", "256") KNNSSD_TS_NEXT("24", "384")
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t}" ::"r"(d), "r"(p), "r"(v), "r"(idesc), "r"(add), "r"(DESC_UPPER), "r"(bar)
                  : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add, uint32_t one) {
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
-                 "r"(idesc), "r"(add), "r"(one)
-                 : "memory");
-}
-__device__ __forceinline__ void commit(uint32_t bar, uint32_t one) {
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(one) : "memory");
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -109,6 +125,7 @@ __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.
 
 #define KNNSSD_R32(X, r) X(r[0]), X(r[1]), X(r[2]), X(r[3]), X(r[4]), X(r[5]), X(r[6]), X(r[7]), X(r[8]), X(r[9]), X(r[10]), X(r[11]), X(r[12]), X(r[13]), X(r[14]), X(r[15]), \
     X(r[16]), X(r[17]), X(r[18]), X(r[19]), X(r[20]), X(r[21]), X(r[22]), X(r[23]), X(r[24]), X(r[25]), X(r[26]), X(r[27]), X(r[28]), X(r[29]), X(r[30]), X(r[31])
+#define KNNSSD_R16(X, r) X(r[0]), X(r[1]), X(r[2]), X(r[3]), X(r[4]), X(r[5]), X(r[6]), X(r[7]), X(r[8]), X(r[9]), X(r[10]), X(r[11]), X(r[12]), X(r[13]), X(r[14]), X(r[15])
 #define KNNSSD_OUT(x) "=r"(x)
 #define KNNSSD_IN(x) "r"(x)
 #define KNNSSD_IO(x) "+r"(x)
@@ -128,23 +145,74 @@ __device__ __forceinline__ void tmem_st(uint32_t t, const uint32_t (&r)[32]) {
                  : "memory");
 }
 
-// What a run has of an item: steps (tiles of KEYS positions) j0 .. of either half; a half without rows, or whose rows end before, has none.
+__device__ __forceinline__ void tmem_st16(uint32_t t, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::KNNSSD_R16(KNNSSD_IN, r), "r"(t)
+                 : "memory");
+}
+
+// ---- pairs of fp32 values: two operations an instruction -------------------------------------------------------------
+__device__ __forceinline__ uint64_t pair_of(uint32_t a, uint32_t b) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(a), "r"(b));
+    return p;
+}
+__device__ __forceinline__ uint64_t pair_of(float a, float b) { return pair_of(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ void split(uint64_t p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 2^x of two values on the multiply-add units: x = n + f with n the nearest whole number (added to 1.5 2^23 it is the sum's low bits), 2^f by a
+// cubic (minimax of the relative error on [-1/2, 1/2] by Lawson's weighted least squares: 7.5e-5, an eighth of what rounding to bf16
+// does at most), and n added to the exponent.  Below 2^-126 it gives 2^-126.
+__device__ __forceinline__ void exp2_cubic(uint64_t x, float &a, float &b) {
+    float x0, x1;
+    split(x, x0, x1);
+    x = pair_of(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+    const uint64_t big = pair_of(12582912.f, 12582912.f), n = add2(x, big), f = add2(x, mul2(add2(n, pair_of(-12582912.f, -12582912.f)), pair_of(-1.f, -1.f)));
+    uint64_t y = fma2(f, pair_of(0.0551716685295105f, 0.0551716685295105f), pair_of(0.2426111251115799f, 0.2426111251115799f));
+    y = fma2(f, y, pair_of(0.6932609677314758f, 0.6932609677314758f));
+    y = fma2(f, y, pair_of(0.9999280571937561f, 0.9999280571937561f));
+    float y0, y1, n0, n1;
+    split(y, y0, y1);
+    split(n, n0, n1);
+    a = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(n0) << 23));
+    b = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(n1) << 23));
+}
+
+// What a run has of an item: n[h] steps of SUB positions from tile j0 on for either half; a half without rows, or whose rows end before, has none.
 struct Job {
-    int from, to, j0, n[2], steps, seen0, tokens;
+    int from, to, j0, n[2], tiles, seen0, tokens;
     bool paired;
     __device__ __forceinline__ Job(const Args &a, const Item<true> &it, long long x0, long long x1) {
         from = cut<KEYS>(it, x0); to = cut<KEYS>(it, x1);
         j0 = from / KEYS;
         tokens = it.tokens();
         seen0 = it.kv - tokens;
-        paired = it.paired();
+        paired = it.r.paired;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int end = paired ? it.kv : min(it.kv, seen0 + (h + 1) * a.tb);
             const bool rows = h == 0 || (paired ? 2 * it.vh + 1 < a.nvh : tokens > a.tb);
-            n[h] = rows && from < to ? max(0, (min(to, end) + KEYS - 1) / KEYS - j0) : 0;
+            n[h] = rows && from < to ? max(0, (min(to, end) + SUB - 1) / SUB - from / SUB) : 0;
         }
-        steps = max(n[0], n[1]);
+        tiles = (max(n[0], n[1]) + KEYS / SUB - 1) / (KEYS / SUB);
     }
 };
 
@@ -207,21 +275,21 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
     using L = Lay<HD>;
     extern __shared__ unsigned char raw[];
     __shared__ Costs<NCOST> costs;
-    __shared__ uint64_t bars[2 + 2 + 2 * L::TILES + 2 + 2 + 2];
+    __shared__ uint64_t bars[2 + 2 + 2 * L::TILES + 4 + 4 + 4];        // s_full, p_full and o_full: [half][buffer]
     __shared__ uint32_t tmem_base;
     __shared__ volatile int quit;
     __shared__ volatile unsigned info[INFO];                         // the 16-position groups of a step's tile that have a page
     const uint32_t smem = (smem_addr(raw) + 1023u) & ~1023u, q_tile = smem, ring = smem + 2 * L::TILE;
     const uint32_t q_full = smem_addr(bars), q_empty = q_full + 16, kv_full = q_empty + 16, kv_empty = kv_full + 8 * L::TILES, s_full = kv_empty + 8 * L::TILES,
-                   p_full = s_full + 16, o_full = p_full + 16;
+                   p_full = s_full + 32, o_full = p_full + 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         quit = 0;
         for (int i = 0; i < 2; ++i) {
             bar_init(q_full + 8 * i, 1); bar_init(q_empty + 8 * i, 1);
-            bar_init(s_full + 8 * i, 2); bar_init(p_full + 8 * i, 4); bar_init(o_full + 8 * i, 1);
+            for (int b = 0; b < 2; ++b) { bar_init(o_full + 8 * (2 * i + b), 1); bar_init(s_full + 8 * (2 * i + b), 2); bar_init(p_full + 8 * (2 * i + b), 4); }
         }
-        for (int i = 0; i < L::TILES; ++i) { bar_init(kv_full + 8 * i, 1); bar_init(kv_empty + 8 * i, 1); }
+        for (int i = 0; i < L::TILES; ++i) { bar_init(kv_full + 8 * i, 1); bar_init(kv_empty + 8 * i, 2); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
@@ -242,11 +310,8 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
     } else {
         Item<true> it = item_at<true>(a, costs, x0);
         if (tid == 0) note_part<KEYS>(a, it, w, W, total, x0, x1);
-        const uint32_t one = elect();
         bool ok = true, more = true;
 
-        if (warp >= SOFT_WARPS) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
         if (warp == LOAD_WARP) {
             // ---- copies ------------------------------------------------------------------------------------------------
             unsigned fills = 0, qfills[2] = {0, 0}, step0 = 0;
@@ -260,8 +325,8 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
             };
             auto put = [&](const CUtensorMap *map, int vh, int j, int page, bool note, unsigned step) {
                 const unsigned slot = fills % L::TILES, turn = fills / L::TILES;
-                ok = ok && bar_wait(kv_empty + 8 * slot, (turn & 1) ^ 1, &quit, a.err, 201);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; return; }
+                if (ok) ok = warp_wait(kv_empty + 8 * slot, (turn & 1) ^ 1, &quit, a.err, 201);
+                if (!ok) return;
                 const uint32_t dst = ring + slot * L::TILE, bar = kv_full + 8 * slot;
                 const int kvh = vh / a.subs;
                 if (PAGED) {
@@ -292,15 +357,15 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
             while (more && ok) {
                 const Job job(a, it, x0, x1);
                 const int v0 = job.paired ? 2 * it.vh : it.vh, v1 = job.paired ? v0 + 1 : v0;
-                if (PAGED && job.steps) { id = page_of(job.j0); next_id = page_of(job.j0 + 1); }
+                if (PAGED && job.tiles) { id = page_of(job.j0); next_id = page_of(job.j0 + 1); }
                 // the first tile's K before q: the ring has room while q waits for the products of the item before
                 auto k_of = [&](int s, int page) {
                     if (!job.paired) put(&kmap, v0, job.j0 + s, page, true, step0 + s);
                 };
                 for (int h = 0; h < 2 && ok; ++h)
                     if (job.n[h]) {
-                        ok = bar_wait(q_empty + 8 * h, (qfills[h] & 1) ^ 1, &quit, a.err, 202);
-                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        ok = warp_wait(q_empty + 8 * h, (qfills[h] & 1) ^ 1, &quit, a.err, 202);
+                        if (!ok) break;
                         if (lane == 0) {
                             const int vh = h ? v1 : v0, h0 = vh / a.subs * (a.H / a.KV) + vh % a.subs * a.gs;
                             const int row = it.r.row0 + it.rb * it.r.tb + (job.paired ? 0 : h * a.tb);
@@ -312,9 +377,9 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                         if (h == 0 && ok) { if (job.paired) put(&kmap, v0, job.j0, id, true, step0); else k_of(0, id); }
                         if (h == 1 && ok) { if (job.paired) put(&kmap, v1, job.j0, id, false, step0); else if (!job.n[0]) k_of(0, id); }
                     }
-                for (int s = 0; s < job.steps && ok; ++s) {
+                for (int s = 0; s < job.tiles && ok; ++s) {
                     const int j = job.j0 + s;
-                    const bool again = s + 1 < job.steps;
+                    const bool again = s + 1 < job.tiles;
                     if (!job.paired) {
                         put(&vmap, v0, j, id, false, 0);
                         if (again && ok) k_of(s + 1, next_id);
@@ -326,41 +391,56 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                     }
                     if (PAGED) { id = next_id; next_id = page_of(j + 2); }
                 }
-                step0 += job.steps;
+                step0 += job.tiles;
                 more = it.next(a) && it.start < x1;
             }
             // every copy has landed and every product has let go of its tile before the block goes
             for (unsigned i = fills > L::TILES ? fills - L::TILES : 0; i < fills; ++i) {
                 const unsigned slot = i % L::TILES, parity = i / L::TILES & 1;
-                if (ok) ok = bar_wait(kv_empty + 8 * slot, parity, &quit, a.err, 203);
+                if (ok) ok = warp_wait(kv_empty + 8 * slot, parity, &quit, a.err, 203);
                 if (!ok)
                     for (unsigned spins = 0; spins < WAIT_LIMIT && !bar_try(kv_full + 8 * slot, parity); ++spins) {}
             }
             for (int h = 0; h < 2; ++h)
                 if (qfills[h]) {
-                    if (ok) ok = bar_wait(q_empty + 8 * h, (qfills[h] - 1) & 1, &quit, a.err, 204);
+                    if (ok) ok = warp_wait(q_empty + 8 * h, (qfills[h] - 1) & 1, &quit, a.err, 204);
                     if (!ok)
                         for (unsigned spins = 0; spins < WAIT_LIMIT && !bar_try(q_full + 8 * h, (qfills[h] - 1) & 1); ++spins) {}
                 }
-        } else if (warp == MMA_WARP) {
+        } else if (warp >= MMA_WARP) {
             // ---- products ------------------------------------------------------------------------------------------------
-            constexpr uint32_t S_DESC = idesc_of(KEYS, false), O_DESC = idesc_of(HD, true);
-            unsigned uses = 0, q_uses[2] = {0, 0}, p_uses[2] = {0, 0}, step0 = 0;
-            auto tile_there = [&](unsigned use) { ok = ok && bar_wait(kv_full + 8 * (use % L::TILES), use / L::TILES & 1, &quit, a.err, 205); return ok; };
-            auto scores = [&](int h, unsigned use) {
-                if (lane == 0) bar_arrive(s_full + 8 * h);           // hands on what the copies' warp noted of the tile
-                fence_after();
-                const uint32_t q = q_tile + h * L::TILE, k = ring + use % L::TILES * L::TILE;
-#pragma unroll
-                for (int i = 0; i < HD / 16; ++i)
-                    mma_ss(tmem + h * KEYS, desc_of(q + (i >> 2) * BAND + (i & 3) * 32), desc_of(k + (i >> 2) * BAND + (i & 3) * 32), S_DESC, i > 0, one);
-                commit(s_full + 8 * h, one);
+            // A warp per half: its own instructions, some 150 a step next to 640 clocks of products, bound the loop where one warp served both.
+            // Of the half two steps are under way: while the softmax works on one, the scores of the other are formed.
+            constexpr uint32_t S_DESC = idesc_of(SUB, false), O_DESC = idesc_of(HD, true), SUB_STEP = SUB * 128 >> 4;
+            const int h = warp - MMA_WARP;
+            const uint32_t q_desc = desc_of(q_tile + h * L::TILE), s_col = tmem + h * KEYS, o_col = tmem + O_COL + h * HD;
+            const uint32_t my_s = s_full + 16 * h, my_p = p_full + 16 * h, my_o = o_full + 16 * h, my_q = q_full + 8 * h, my_q_empty = q_empty + 8 * h;
+            unsigned slot = 0, phase = 0, q_phase = 0, step0 = 0;    // slot, phase: the ring's next tile
+            unsigned sb = 0, vbuf = 0, p_phase = 0;                  // the buffers that scores go to and p comes from, p's phase
+            // Either half goes through every tile of the ring, waits for it and lets it go, whether it has a use for it or not: a half that left the
+            // other's tiles out could be a turn of the ring ahead, where a barrier's parity no longer tells one phase from the next.
+            unsigned walked = 0;
+            auto there = [&]() { if (ok) ok = warp_wait(kv_full + 8 * slot, phase, &quit, a.err, 205); };
+            auto onward = [&]() {
+                ++walked;
+                if (++slot == L::TILES) { slot = 0; phase ^= 1; }
+            };
+            auto pass = [&](unsigned tiles) {
+                for (; tiles > 0 && ok; --tiles) {
+                    there();
+                    if (ok && lane == 0) bar_arrive(kv_empty + 8 * slot);
+                    onward();
+                }
+            };
+            auto take = [&](uint32_t &tile, uint32_t &bar) {
+                there();
+                tile = ring + slot * L::TILE;
+                bar = kv_empty + 8 * slot;
+                onward();
             };
             // What lies behind the last position that the block sees, and what has no page, must be zero in V: its p is 0, and 0 times what happens
-            // to lie there need not be.
-            auto clean = [&](unsigned use, int valid, unsigned groups) {
-                if (valid >= KEYS && groups == 0xffu) return;
-                const uint32_t v = ring + use % L::TILES * L::TILE;
+            // to lie there need not be.  (Where the halves share the tile both do it.)
+            auto clean = [&](uint32_t v, int valid, unsigned groups) {
                 for (int i = lane; i < KEYS * 8; i += 32) {
                     const int row = i >> 3;
                     if (row < valid && (groups >> (row >> 4) & 1)) continue;
@@ -371,54 +451,60 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
             };
-            auto values = [&](int h, unsigned use, bool add) {
-                ok = ok && bar_wait(p_full + 8 * h, p_uses[h]++ & 1, &quit, a.err, 206);
-                if (!ok) return;
-                fence_after();
-                const uint32_t v = ring + use % L::TILES * L::TILE;
-#pragma unroll
-                for (int i = 0; i < KEYS / 16; ++i)
-                    mma_ts(tmem + O_COL + h * HD, tmem + h * KEYS + 8 * i, desc_of(v + i * 2048), O_DESC, add || i > 0, one);
-                commit(o_full + 8 * h, one);
-            };
-            auto let_go = [&](unsigned use) { commit(kv_empty + 8 * (use % L::TILES), one); };
             while (more && ok) {
                 const Job job(a, it, x0, x1);
-                unsigned k_use[2] = {0, 0}, v_use[2] = {0, 0};
-                auto score_step = [&](int h, int s) {
-                    if (job.paired || h == 0 || job.n[0] <= s) k_use[h] = uses++; else k_use[h] = k_use[0];
-                    if (s == 0) ok = ok && bar_wait(q_full + 8 * h, q_uses[h]++ & 1, &quit, a.err, 207);
-                    if (!ok || !tile_there(k_use[h])) { ok = false; return; }
-                    scores(h, k_use[h]);
-                    if (s + 1 == job.n[h]) commit(q_empty + 8 * h, one);
-                    if (job.paired || h == 1 || job.n[1] <= s) let_go(k_use[h]);
+                const int n = h ? job.n[1] : job.n[0], other = h ? job.n[0] : job.n[1], T = job.tiles;
+                // Tiles come as K0 V0 K1 V1 .., where the halves have tiles of their own (A, B) as KA0 KB0 VA0 KA1 VB0 KB1 VA1 ..
+                const bool own = job.paired && n > 0 && other > 0;
+                walked = 0;
+                uint32_t k = 0, k_bar = 0, v = 0, v_bar = 0;
+                auto scores = [&](int u) {
+                    if ((u & 1) == 0) {
+                        if (own && h && u == 0) pass(1);
+                        take(k, k_bar);
+                    }
+                    if (!ok) return;
+                    const uint32_t bar = my_s + 8 * sb;
+                    if (lane == 0) bar_arrive(bar);                  // hands on what the copies' warp noted of the tile
+                    fence_after();
+                    mma_scores<HD>(s_col + sb * SUB, q_desc, desc_of(k) + (u & 1) * SUB_STEP, S_DESC, bar);
+                    sb ^= 1;
+                    if (u + 1 == n) commit(my_q_empty);
+                    if ((u & 1) || u + 1 == n) commit(k_bar);
                 };
-                for (int h = 0; h < 2 && ok; ++h)
-                    if (job.n[h]) score_step(h, 0);
-                for (int s = 0; s < job.steps && ok; ++s) {
-                    const int valid = it.kv - (job.j0 + s) * KEYS;
-                    for (int h = 0; h < 2 && ok; ++h) {
-                        if (job.n[h] <= s) continue;
-                        const bool own_tile = job.paired || h == 0 || job.n[0] <= s;
-                        if (own_tile) v_use[h] = uses++; else v_use[h] = v_use[0];
-                        if (!tile_there(v_use[h])) break;
-                        if (own_tile) clean(v_use[h], valid, PAGED ? info[(step0 + s) % INFO] : 0xffu);
-                        values(h, v_use[h], s > 0);
+                if (n > 0) {
+                    if (ok) ok = warp_wait(my_q, q_phase, &quit, a.err, 207);
+                    q_phase ^= 1;
+                    scores(0);
+                    if (n > 1 && ok) scores(1);
+                    for (int u = 0; u < n && ok; ++u) {
+                        if ((u & 1) == 0) {
+                            const int t = u >> 1;
+                            if (own) pass(h ? (t == T - 1 ? 1 : 2) : (t == 0 ? 1 : 2));
+                            take(v, v_bar);
+                            const int valid = it.kv - (job.j0 + t) * KEYS;
+                            const unsigned groups = PAGED ? info[(step0 + t) % INFO] : 0xffu;
+                            if (ok && (valid < KEYS || groups != 0xffu)) clean(v, valid, groups);
+                        }
+                        if (ok) ok = warp_wait(my_p + 8 * vbuf, p_phase, &quit, a.err, 206);
                         if (!ok) break;
-                        if (job.paired || h == 1 || job.n[1] <= s) let_go(v_use[h]);
-                        if (s + 1 < job.n[h]) score_step(h, s + 1);
+                        fence_after();
+                        mma_values(o_col, s_col + vbuf * SUB, desc_of(v) + (u & 1) * SUB_STEP, O_DESC, u > 0, my_o + 8 * vbuf);
+                        p_phase ^= vbuf;
+                        vbuf ^= 1;
+                        if ((u & 1) || u + 1 == n) commit(v_bar);
+                        if (u + 2 < n) scores(u + 2);
                     }
                 }
-                step0 += job.steps;
+                pass((own ? 4 : 2) * T - walked);
+                step0 += job.tiles;
                 more = it.next(a) && it.start < x1;
             }
-        }
         } else {
             // ---- softmax ---------------------------------------------------------------------------------------------------
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
             const int h = warp >> 2, r = h * HALF_ROWS + (warp & 3) * 32 + lane;
-            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), s_at = lanes + h * KEYS, o_at = lanes + O_COL + h * HD;
-            unsigned s_uses = 0, o_uses = 0, step0 = 0;
+            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), o_at = lanes + O_COL + h * HD;
+            unsigned done = 0, step0 = 0;                            // steps of this half
             while (more && ok) {
                 const Job job(a, it, x0, x1);
                 int token, head;
@@ -426,43 +512,45 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                 const int last = token >= 0 ? job.seen0 + token : -1, first_last = job.seen0 + (job.paired ? 0 : h * a.tb);
                 const size_t row = (size_t)(it.r.row0 + it.rb * it.r.tb + (token < 0 ? 0 : token)) * a.H + head;
                 const bool live = __any_sync(0xffffffffu, token >= 0);
+                const int steps = h ? job.n[1] : job.n[0];
                 float m = -INFINITY, l = 0.f;
-                for (int s = 0; s < job.n[h] && ok; ++s) {
-                    const int k0 = (job.j0 + s) * KEYS;
-                    ok = bar_wait(s_full + 8 * h, s_uses++ & 1, &quit, a.err, 208);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                for (int u = 0; u < steps && ok; ++u, ++done) {
+                    const uint32_t bar = 8 * (2 * h + (done & 1)), s_at = lanes + h * KEYS + (done & 1) * SUB;
+                    const int k0 = job.from + u * SUB;
+                    ok = warp_wait(s_full + bar, done >> 1 & 1, &quit, a.err, 208);
+                    if (!ok) break;
                     if (!live) {                                     // none of the warp's rows is anyone's: what is in P there stays there
                         __syncwarp();
-                        if (lane == 0) bar_arrive(p_full + 8 * h);
-                        ++o_uses;
+                        if (lane == 0) bar_arrive(p_full + bar);
                         continue;
                     }
                     fence_after();
-                    uint32_t x[4][32];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ld(s_at + 32 * i, x[i]);
+                    uint32_t x[2][32];
+                    tmem_ld(s_at, x[0]);
+                    tmem_ld(s_at + 32, x[1]);
                     wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) settle(x[i]);
-                    const unsigned groups = PAGED ? info[(step0 + s) % INFO] : 0xffu;
-                    const bool ragged = k0 + KEYS - 1 > first_last || groups != 0xffu;
+                    settle(x[0]);
+                    settle(x[1]);
+                    const unsigned groups = PAGED ? info[(step0 + (u >> 1)) % INFO] >> (4 * (u & 1)) & 15u : 15u;
+                    const bool ragged = k0 + SUB - 1 > first_last || groups != 15u;
+                    const int see = last - k0;                       // the row sees keys 0 .. see of the step
                     if (ragged) {
-                        const int see = last - k0;                   // the row sees keys 0 .. see of the tile
 #pragma unroll
-                        for (int i = 0; i < KEYS; ++i)
+                        for (int i = 0; i < SUB; ++i)
                             if (i > see || !(groups >> (i >> 4) & 1)) x[i >> 5][i & 31] = 0xff800000u;
                     }
-                    float top = -INFINITY;
+                    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < KEYS; ++i) top = fmaxf(top, __uint_as_float(x[i >> 5][i & 31]));
+                    for (int i = 0; i < SUB; i += 2) tops[(i >> 1) & 3] = max3(tops[(i >> 1) & 3], __uint_as_float(x[i >> 5][i & 31]), __uint_as_float(x[i >> 5][(i & 31) + 1]));
+                    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     const float grown = top == -INFINITY ? -INFINITY : top * a.scale_log2;
                     const bool over = grown > m + GROWTH;            // the first positions a row sees: m is -inf
                     if (__any_sync(0xffffffffu, over)) {
                         const float f = over ? exp2_approx(m - grown) : 1.f;
                         if (over) { m = grown; l *= f; }
-                        if (s > 0) {
-                            ok = bar_wait(o_full + 8 * h, (o_uses - 1) & 1, &quit, a.err, 209);
-                            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        if (u > 0) {
+                            ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a.err, 209);
+                            if (!ok) break;
                             fence_after();
 #pragma unroll
                             for (int c = 0; c < HD / 32; ++c) {
@@ -477,46 +565,61 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                         }
                     }
                     const float base = m == -INFINITY ? 0.f : m;
-                    uint32_t p[2][32];
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint64_t sums[2] = {0, 0};
+                    const uint64_t scale2 = pair_of(a.scale_log2, a.scale_log2), base2 = pair_of(-base, -base);
+                    uint32_t p[32];
+                    if (!ragged) {
 #pragma unroll
-                    for (int i = 0; i < KEYS; i += 2) {
-                        float u = exp2_approx(fmaf(__uint_as_float(x[i >> 5][i & 31]), a.scale_log2, -base));
-                        float v = exp2_approx(fmaf(__uint_as_float(x[(i + 1) >> 5][(i + 1) & 31]), a.scale_log2, -base));
-                        if (ragged) {                                // also where scale is 0
-                            const int see = last - k0;
-                            const bool gone = !(groups >> (i >> 4) & 1);
-                            if (i > see || gone) u = 0.f;
-                            if (i + 1 > see || gone) v = 0.f;
+                        for (int i = 0; i < SUB; i += 2) {
+                            const uint64_t e = fma2(pair_of(x[i >> 5][i & 31], x[i >> 5][(i & 31) + 1]), scale2, base2);
+                            float v0, v1;
+                            if ((i >> 1) % CUBIC_OF < CUBIC) {
+                                exp2_cubic(e, v0, v1);
+                            } else {
+                                split(e, v0, v1);
+                                v0 = exp2_approx(v0);
+                                v1 = exp2_approx(v1);
+                            }
+                            sums[(i >> 1) & 1] = add2(sums[(i >> 1) & 1], pair_of(v0, v1));
+                            p[i >> 1] = cvt_bf16x2(v0, v1);
                         }
-                        sum[(i >> 1) & 3] += u + v;
-                        p[i >> 6][(i >> 1) & 31] = cvt_bf16x2(u, v);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < SUB; i += 2) {           // zeros also where scale is 0
+                            const bool gone = !(groups >> (i >> 4) & 1);
+                            float v0 = exp2_approx(fmaf(__uint_as_float(x[i >> 5][i & 31]), a.scale_log2, -base));
+                            float v1 = exp2_approx(fmaf(__uint_as_float(x[i >> 5][(i & 31) + 1]), a.scale_log2, -base));
+                            if (i > see || gone) v0 = 0.f;
+                            if (i + 1 > see || gone) v1 = 0.f;
+                            sums[(i >> 1) & 1] = add2(sums[(i >> 1) & 1], pair_of(v0, v1));
+                            p[i >> 1] = cvt_bf16x2(v0, v1);
+                        }
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    tmem_st(s_at, p[0]);
-                    tmem_st(s_at + 32, p[1]);
+                    tmem_st(s_at, p);
+                    float sum0, sum1;
+                    split(add2(sums[0], sums[1]), sum0, sum1);
+                    l += sum0 + sum1;
                     wait_st();
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(p_full + 8 * h);
-                    ++o_uses;
+                    if (lane == 0) bar_arrive(p_full + bar);
                 }
                 if (!ok) break;
                 // ---- the row's end
                 const bool whole = job.from == 0 && job.to == it.kv;
-                if (job.n[h]) {
-                    ok = bar_wait(o_full + 8 * h, (o_uses - 1) & 1, &quit, a.err, 210);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                if (steps) {
+                    ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a.err, 210);
+                    if (!ok) break;
                     fence_after();
                 }
-                if (live && (job.n[h] || (job.from < job.to && !whole))) {
+                if (live && (steps || (job.from < job.to && !whole))) {
                     const float f = whole ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
                     const size_t slot = ((size_t)w * SLOTS + (job.from > 0 ? 0 : 1)) * ROWS + r;
                     bool odd = false;
 #pragma unroll
                     for (int c = 0; c < HD / 32; ++c) {
                         uint32_t o[32];
-                        if (job.n[h]) {
+                        if (steps) {
                             tmem_ld(o_at + 32 * c, o);
                             wait_ld();
                             settle(o);
@@ -546,10 +649,10 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                         }
                     }
                     if (token >= 0 && !whole) a.ml[slot] = make_float2(m, l);
-                    if (odd && token >= 0) mend_row<HD, PAGED>(a, it.b, it.r.row0, job.from, min(job.to, (job.j0 + job.n[h]) * KEYS), it.kv, it.r.row0 + it.rb * it.r.tb + token, head, last, whole, slot);
+                    if (odd && token >= 0) mend_row<HD, PAGED>(a, it.b, it.r.row0, job.from, min(job.to, job.from + steps * SUB), it.kv, it.r.row0 + it.rb * it.r.tb + token, head, last, whole, slot);
                     fence_before();
                 }
-                step0 += job.steps;
+                step0 += job.tiles;
                 more = it.next(a) && it.start < x1;
             }
         }
