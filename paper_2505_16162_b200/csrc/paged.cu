@@ -166,7 +166,7 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
     if (n_rows < 0 || n_requests < 1 || max_fresh < 0 || !std::isfinite(scale) || scale < 0.f) return KNNSSD_ERR_INVALID_ARG;
     if (knnssd_status st = check_heads(dtype, cache_dtype, n_heads, n_kv_heads, head_dim); st != KNNSSD_OK) return st;
     if (knnssd_status st = check_pages(page_size, max_pages, n_pages); st != KNNSSD_OK) return st;
-    if (n_rows > INT_MAX / 2) return KNNSSD_ERR_CAPACITY;
+    if (n_rows > INT_MAX / 2 || (long long)n_rows * n_heads > INT_MAX) return KNNSSD_ERR_CAPACITY;
     if (n_rows == 0) return KNNSSD_OK;
     if (!q_dev || !k_pages_dev || !v_pages_dev || !table_dev || !lens_dev || !row_start_dev || !out_dev) return KNNSSD_ERR_INVALID_ARG;
     if (q_stride < (long long)n_heads * head_dim || q_stride % (dtype ? 8 : 4) != 0 || !aligned16(q_dev) || !aligned16(k_pages_dev) || !aligned16(v_pages_dev) || !aligned16(out_dev))
@@ -192,7 +192,7 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
                                       void *cuda_stream) {
     if (n_rows < 0 || n_requests < 1 || !std::isfinite(scale) || scale < 0.f) return KNNSSD_ERR_INVALID_ARG;
     if (knnssd_status st = check_heads(dtype, dtype, n_heads, n_kv_heads, head_dim); st != KNNSSD_OK) return st;
-    if (n_rows > INT_MAX / 2) return KNNSSD_ERR_CAPACITY;
+    if (n_rows > INT_MAX / 2 || (long long)n_rows * n_heads > INT_MAX) return KNNSSD_ERR_CAPACITY;
     if (n_rows == 0) return KNNSSD_OK;
     if (!q_dev || !k_dev || !v_dev || !row_start_dev || !out_dev) return KNNSSD_ERR_INVALID_ARG;
     const int per16 = dtype ? 8 : 4;

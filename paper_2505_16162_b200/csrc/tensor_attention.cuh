@@ -196,6 +196,21 @@ __device__ __forceinline__ void exp2_cubic(uint64_t x, float &a, float &b) {
     b = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(n1) << 23));
 }
 
+// Lane 4 i + j has row j of a 4 x 4 square of 16-byte pieces; afterwards it has column j.
+__device__ __forceinline__ void turn4(uint4 (&v)[4], int lane) {
+    auto swap = [&](uint4 &a, uint4 &b, int by) {                    // the lanes with the bit give a and take into it, the others b
+        const bool up = lane & by;
+        uint4 t = up ? a : b;
+        t.x = __shfl_xor_sync(0xffffffffu, t.x, by); t.y = __shfl_xor_sync(0xffffffffu, t.y, by);
+        t.z = __shfl_xor_sync(0xffffffffu, t.z, by); t.w = __shfl_xor_sync(0xffffffffu, t.w, by);
+        if (up) a = t; else b = t;
+    };
+    swap(v[0], v[1], 1);
+    swap(v[2], v[3], 1);
+    swap(v[0], v[2], 2);
+    swap(v[1], v[3], 2);
+}
+
 // What a run has of an item: n[h] steps of SUB positions from tile j0 on for either half; a half without rows, or whose rows end before, has none.
 struct Job {
     int from, to, j0, n[2], tiles, seen0, tokens;
@@ -505,12 +520,17 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
             const int h = warp >> 2, r = h * HALF_ROWS + (warp & 3) * 32 + lane;
             const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), o_at = lanes + O_COL + h * HD;
             unsigned done = 0, step0 = 0;                            // steps of this half
+            const int rr = r % HALF_ROWS, my_head = rr % a.gs, my_token = rr / a.gs < a.tb ? rr / a.gs : -1, G = a.H / a.KV;      // as place_of
             while (more && ok) {
                 const Job job(a, it, x0, x1);
-                int token, head;
-                place_of<true, ROWS>(a, job.tokens, it.vh, job.paired, r, token, head);
+                int token = my_token + (job.paired ? 0 : h * a.tb), head;
+                {
+                    const int v = job.paired ? 2 * it.vh + h : it.vh, kvh = a.subs == 1 ? v : v / a.subs, hh = (a.subs == 1 ? 0 : v % a.subs * a.gs) + my_head;
+                    if (my_token < 0 || token >= job.tokens || v >= a.nvh || hh >= G) token = -1;
+                    head = kvh * G + hh;
+                }
                 const int last = token >= 0 ? job.seen0 + token : -1, first_last = job.seen0 + (job.paired ? 0 : h * a.tb);
-                const size_t row = (size_t)(it.r.row0 + it.rb * it.r.tb + (token < 0 ? 0 : token)) * a.H + head;
+                const int row = (it.r.row0 + it.rb * it.r.tb + (token < 0 ? 0 : token)) * a.H + head;
                 const bool live = __any_sync(0xffffffffu, token >= 0);
                 const int steps = h ? job.n[1] : job.n[0];
                 float m = -INFINITY, l = 0.f;
@@ -605,7 +625,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                     if (lane == 0) bar_arrive(p_full + bar);
                 }
                 if (!ok) break;
-                // ---- the row's end
+                // ---- the rows' ends
                 const bool whole = job.from == 0 && job.to == it.kv;
                 if (steps) {
                     ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a.err, 210);
@@ -614,8 +634,16 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                 }
                 if (live && (steps || (job.from < job.to && !whole))) {
                     const float f = whole ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
-                    const size_t slot = ((size_t)w * SLOTS + (job.from > 0 ? 0 : 1)) * ROWS + r;
-                    bool odd = false;
+                    const size_t slot = ((size_t)w * SLOTS + (job.from > 0 ? 0 : 1)) * ROWS;
+                    // Lane 4 i + j takes the j-th 16 bytes of each of the rows 4 i .. 4 i + 3: a store of the warp is eight runs of 64 bytes, where a row
+                    // per lane is 32 half sectors (the end of an item took 9000 clocks, its stores in the way of the other warps').
+                    int at[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        at[i] = __shfl_sync(0xffffffffu, whole ? row : r, (lane & ~3) + i);
+                        if (__shfl_sync(0xffffffffu, token, (lane & ~3) + i) < 0) at[i] = -1;
+                    }
+                    float bad[2] = {0.f, 0.f};                       // 0 times the sums: not 0 where one is not finite
 #pragma unroll
                     for (int c = 0; c < HD / 32; ++c) {
                         uint32_t o[32];
@@ -627,29 +655,40 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
 #pragma unroll
                             for (int i = 0; i < 32; ++i) o[i] = 0u;
                         }
-                        if (token < 0) continue;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) odd |= (o[i] & 0x7f800000u) == 0x7f800000u;
+                        for (int i = 0; i < 32; ++i) bad[i & 1] = fmaf(__uint_as_float(o[i]), 0.f, bad[i & 1]);
                         if (whole) {
-                            bf16_t *d = static_cast<bf16_t *>(a.out) + row * HD + 32 * c;
+                            uint4 v[4];
 #pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                uint4 v;
-                                v.x = cvt_bf16x2(__uint_as_float(o[i]) * f, __uint_as_float(o[i + 1]) * f);
-                                v.y = cvt_bf16x2(__uint_as_float(o[i + 2]) * f, __uint_as_float(o[i + 3]) * f);
-                                v.z = cvt_bf16x2(__uint_as_float(o[i + 4]) * f, __uint_as_float(o[i + 5]) * f);
-                                v.w = cvt_bf16x2(__uint_as_float(o[i + 6]) * f, __uint_as_float(o[i + 7]) * f);
-                                *reinterpret_cast<uint4 *>(d + i) = v;
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t *p = o + 8 * i;
+                                v[i].x = cvt_bf16x2(__uint_as_float(p[0]) * f, __uint_as_float(p[1]) * f);
+                                v[i].y = cvt_bf16x2(__uint_as_float(p[2]) * f, __uint_as_float(p[3]) * f);
+                                v[i].z = cvt_bf16x2(__uint_as_float(p[4]) * f, __uint_as_float(p[5]) * f);
+                                v[i].w = cvt_bf16x2(__uint_as_float(p[6]) * f, __uint_as_float(p[7]) * f);
                             }
-                        } else {
-                            float *d = a.o + slot * HD + 32 * c;
+                            turn4(v, lane);
 #pragma unroll
-                            for (int i = 0; i < 32; i += 4)
-                                *reinterpret_cast<uint4 *>(d + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                            for (int i = 0; i < 4; ++i)
+                                if (at[i] >= 0) *reinterpret_cast<uint4 *>(static_cast<bf16_t *>(a.out) + (size_t)at[i] * HD + 32 * c + 8 * (lane & 3)) = v[i];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                uint4 v[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) v[i] = make_uint4(o[16 * e + 4 * i], o[16 * e + 4 * i + 1], o[16 * e + 4 * i + 2], o[16 * e + 4 * i + 3]);
+                                turn4(v, lane);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    if (at[i] >= 0) *reinterpret_cast<uint4 *>(a.o + (slot + at[i]) * HD + 32 * c + 16 * e + 4 * (lane & 3)) = v[i];
+                            }
                         }
                     }
-                    if (token >= 0 && !whole) a.ml[slot] = make_float2(m, l);
-                    if (odd && token >= 0) mend_row<HD, PAGED>(a, it.b, it.r.row0, job.from, min(job.to, job.from + steps * SUB), it.kv, it.r.row0 + it.rb * it.r.tb + token, head, last, whole, slot);
+                    if (token >= 0 && !whole) a.ml[slot + r] = make_float2(m, l);
+                    __syncwarp();
+                    const float odd = bad[0] + bad[1];
+                    if (odd != 0.f && token >= 0)
+                        mend_row<HD, PAGED>(a, it.b, it.r.row0, job.from, min(job.to, job.from + steps * SUB), it.kv, it.r.row0 + it.rb * it.r.tb + token, head, last, whole, slot + r);
                     fence_before();
                 }
                 step0 += job.tiles;
