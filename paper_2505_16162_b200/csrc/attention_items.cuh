@@ -139,7 +139,7 @@ template <bool HALVES, int N> __device__ __forceinline__ Item<HALVES> item_at(co
 }
 
 // The run of worker w of W, and where position x cuts an item: at the next multiple of TP of it.
-__device__ __forceinline__ long long run_start(long long total, int w, int W) { return total / W * w + total % W * w / W; }
+__device__ __forceinline__ long long run_start(long long total, int w, int W) { return min(total, ((total + W - 1) / W) * w); }
 template <int TP, bool HALVES> __device__ __forceinline__ int cut(const Item<HALVES> &it, long long x) {
     return (int)(x <= it.start ? 0 : min((x - it.start + TP - 1) & ~(long long)(TP - 1), (long long)it.kv));
 }

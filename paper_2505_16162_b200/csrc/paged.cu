@@ -105,6 +105,9 @@ template <int HD> void launch_rotary(const pages::RotaryArgs &a, int dtype, int 
     else launch_chained(pages::rotary_store_kernel<HD, float, float>, grid, block, 0, s, a);
 }
 
+// The scale of scores in powers of two.  A scale of zero (equal weights) is taken as next to nothing: what a row does not see is -inf times it.
+float log2_scale(float scale) { return scale > 1e-36f ? scale * 1.4426950408889634f : 1e-36f; }
+
 // Types and head counts that the attention operators and the store share.
 knnssd_status check_heads(int dtype, int cache_dtype, int n_heads, int n_kv_heads, int head_dim) {
     if ((dtype != 0 && dtype != 1) || (cache_dtype != 0 && cache_dtype != 1) || n_heads < 1 || n_kv_heads < 1) return KNNSSD_ERR_INVALID_ARG;
@@ -177,7 +180,7 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
     a.table = table_dev; a.max_pages = max_pages; a.n_pages = n_pages;
     while ((1 << a.page_shift) < page_size) ++a.page_shift;
     a.lens = lens_dev; a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_log2 = log2_scale(scale);
     a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     if ((long long)n_pages * page_size * n_kv_heads > INT_MAX) return KNNSSD_ERR_CAPACITY;
@@ -204,7 +207,7 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
     a.q = q_dev; a.out = out_dev; a.q_stride = q_stride;
     a.k = k_dev; a.v = v_dev; a.k_stride = k_stride; a.v_stride = v_stride;
     a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_log2 = log2_scale(scale);
     a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {

@@ -168,11 +168,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -180,12 +175,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 // 2^x of two values on the multiply-add units: x = n + f with n the nearest whole number (added to 1.5 2^23 it is the sum's low bits), 2^f by a
 // cubic (minimax of the relative error on [-1/2, 1/2] by Lawson's weighted least squares: 7.5e-5, an eighth of what rounding to bf16
-// does at most), and n added to the exponent.  Below 2^-126 it gives 2^-126.
+// does at most), and n added to the exponent.  Below 2^-126 it gives 2^-126: next to nothing, but not nothing.
 __device__ __forceinline__ void exp2_cubic(uint64_t x, float &a, float &b) {
     float x0, x1;
     split(x, x0, x1);
     x = pair_of(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-    const uint64_t big = pair_of(12582912.f, 12582912.f), n = add2(x, big), f = add2(x, mul2(add2(n, pair_of(-12582912.f, -12582912.f)), pair_of(-1.f, -1.f)));
+    const uint64_t n = add2(x, pair_of(12582912.f, 12582912.f)), f = fma2(add2(n, pair_of(-12582912.f, -12582912.f)), pair_of(-1.f, -1.f), x);
     uint64_t y = fma2(f, pair_of(0.0551716685295105f, 0.0551716685295105f), pair_of(0.2426111251115799f, 0.2426111251115799f));
     y = fma2(f, y, pair_of(0.6932609677314758f, 0.6932609677314758f));
     y = fma2(f, y, pair_of(0.9999280571937561f, 0.9999280571937561f));
@@ -329,7 +324,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
 
         if (warp == LOAD_WARP) {
             // ---- copies ------------------------------------------------------------------------------------------------
-            unsigned fills = 0, qfills[2] = {0, 0}, step0 = 0;
+            unsigned fills = 0, slot = 0, turn_of = 0, qfills[2] = {0, 0}, step0 = 0;      // slot, turn_of: the ring's next tile
             const int piece = PAGED ? min(1 << a.page_shift, KEYS) : KEYS, pieces = KEYS / piece;
             int id = -1, next_id = -1;                               // lane i: the page of piece i of the tile, of the one behind it
             auto page_of = [&](int j) {
@@ -338,75 +333,75 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                 const int p = __ldg(a.table + (size_t)it.b * a.max_pages + (pos >> a.page_shift));
                 return p < a.n_pages ? p : -1;
             };
-            auto put = [&](const CUtensorMap *map, int vh, int j, int page, bool note, unsigned step) {
-                const unsigned slot = fills % L::TILES, turn = fills / L::TILES;
-                if (ok) ok = warp_wait(kv_empty + 8 * slot, (turn & 1) ^ 1, &quit, a.err, 201);
-                if (!ok) return;
-                const uint32_t dst = ring + slot * L::TILE, bar = kv_full + 8 * slot;
-                const int kvh = vh / a.subs;
-                if (PAGED) {
-                    const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
-                    if (lane == 0) {
-                        if (note) {
-                            unsigned groups = 0;
-                            for (int i = 0; i < pieces; ++i)
-                                if (there >> i & 1) groups |= ((1u << (piece / 16)) - 1) << (i * (piece / 16));
-                            info[step % INFO] = groups;
-                        }
-                        bar_expect(bar, __popc(there) * piece * HD * 2);
-                    }
-                    __syncwarp();
-                    if (page >= 0) {
-                        const int in_page = (j * KEYS + lane * piece) & ((1 << a.page_shift) - 1);
-                        const int y = ((page * a.KV + kvh) << a.page_shift) + in_page;
-#pragma unroll
-                        for (int b = 0; b < L::BANDS; ++b) tma_2d(dst + b * BAND + lane * piece * 128, map, 64 * b, y, bar);
-                    }
-                } else if (lane == 0) {
-                    bar_expect(bar, L::TILE);
-#pragma unroll
-                    for (int b = 0; b < L::BANDS; ++b) tma_3d(dst + b * BAND, map, 64 * b, kvh, it.r.row0 + j * KEYS, bar);
-                }
-                ++fills;
-            };
             while (more && ok) {
                 const Job job(a, it, x0, x1);
-                const int v0 = job.paired ? 2 * it.vh : it.vh, v1 = job.paired ? v0 + 1 : v0;
-                if (PAGED && job.tiles) { id = page_of(job.j0); next_id = page_of(job.j0 + 1); }
-                // the first tile's K before q: the ring has room while q waits for the products of the item before
-                auto k_of = [&](int s, int page) {
-                    if (!job.paired) put(&kmap, v0, job.j0 + s, page, true, step0 + s);
-                };
-                for (int h = 0; h < 2 && ok; ++h)
-                    if (job.n[h]) {
-                        ok = warp_wait(q_empty + 8 * h, (qfills[h] & 1) ^ 1, &quit, a.err, 202);
+                // tiles in the order of their use (see the products)
+                const bool own = job.paired && job.n[0] > 0 && job.n[1] > 0;
+                const int T = job.tiles, total_tiles = (own ? 4 : 2) * T;
+                if (PAGED && T) { id = page_of(job.j0); next_id = page_of(job.j0 + 1); }
+#pragma unroll 1
+                for (int i = 0; i < total_tiles && ok; ++i) {
+                    // half i's q before tile i: the first K is on its way while q waits for the products of the item before
+                    if (i < 2 && (i ? job.n[1] : job.n[0]) > 0) {
+                        ok = warp_wait(q_empty + 8 * i, (qfills[i] & 1) ^ 1, &quit, a.err, 202);
                         if (!ok) break;
                         if (lane == 0) {
-                            const int vh = h ? v1 : v0, h0 = vh / a.subs * (a.H / a.KV) + vh % a.subs * a.gs;
-                            const int row = it.r.row0 + it.rb * it.r.tb + (job.paired ? 0 : h * a.tb);
-                            bar_expect(q_full + 8 * h, a.tb * a.gs * HD * 2);
+                            const int vh = job.paired ? 2 * it.vh + i : it.vh, h0 = vh / a.subs * (a.H / a.KV) + vh % a.subs * a.gs;
+                            const int row = it.r.row0 + it.rb * it.r.tb + (job.paired ? 0 : i * a.tb);
+                            bar_expect(q_full + 8 * i, a.tb * a.gs * HD * 2);
 #pragma unroll
-                            for (int b = 0; b < L::BANDS; ++b) tma_3d(q_tile + h * L::TILE + b * BAND, &qmap, 64 * b, h0, row, q_full + 8 * h);
+                            for (int b = 0; b < L::BANDS; ++b) tma_3d(q_tile + i * L::TILE + b * BAND, &qmap, 64 * b, h0, row, q_full + 8 * i);
                         }
-                        ++qfills[h];
-                        if (h == 0 && ok) { if (job.paired) put(&kmap, v0, job.j0, id, true, step0); else k_of(0, id); }
-                        if (h == 1 && ok) { if (job.paired) put(&kmap, v1, job.j0, id, false, step0); else if (!job.n[0]) k_of(0, id); }
+                        ++qfills[i];
                     }
-                for (int s = 0; s < job.tiles && ok; ++s) {
-                    const int j = job.j0 + s;
-                    const bool again = s + 1 < job.tiles;
-                    if (!job.paired) {
-                        put(&vmap, v0, j, id, false, 0);
-                        if (again && ok) k_of(s + 1, next_id);
+                    bool is_k, second = false;
+                    int t;
+                    if (own) {
+                        const int r = (i - 2) & 3;
+                        t = (i - 2) >> 2;
+                        const bool end = t == T - 1;                 // V of both halves, no K behind them
+                        is_k = i < 2 || (!end && (r & 1));
+                        second = i < 2 ? i == 1 : end ? r == 1 : r >= 2;
+                        t = i < 2 ? 0 : t + is_k;
                     } else {
-                        put(&vmap, v0, j, id, false, 0);
-                        if (again && ok) put(&kmap, v0, j + 1, next_id, true, step0 + s + 1);
-                        if (job.n[1] && ok) put(&vmap, v1, j, id, false, 0);
-                        if (job.n[1] && again && ok) put(&kmap, v1, j + 1, next_id, false, 0);
+                        is_k = !(i & 1);
+                        t = i >> 1;
                     }
-                    if (PAGED) { id = next_id; next_id = page_of(j + 2); }
+                    const bool ahead = is_k && t > 0;                // K of the tile behind the one whose V goes by
+                    ok = warp_wait(kv_empty + 8 * slot, (turn_of & 1) ^ 1, &quit, a.err, 201);
+                    if (!ok) break;
+                    const uint32_t dst = ring + slot * L::TILE, bar = kv_full + 8 * slot;
+                    const int vh = job.paired ? 2 * it.vh + second : it.vh, kvh = a.subs == 1 ? vh : vh / a.subs;
+                    const CUtensorMap *map = is_k ? &kmap : &vmap;
+                    if (PAGED) {
+                        const int page = ahead ? next_id : id;
+                        const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
+                        if (lane == 0) {
+                            if (is_k && !second) {
+                                unsigned groups = 0;
+                                const unsigned each = (1u << (piece / 16)) - 1;
+                                for (int g = 0; g < pieces; ++g)
+                                    if (there >> g & 1) groups |= each << (g * (piece / 16));
+                                info[(step0 + t) % INFO] = groups;
+                            }
+                            bar_expect(bar, __popc(there) * piece * HD * 2);
+                        }
+                        __syncwarp();
+                        if (page >= 0) {
+                            const int y = ((page * a.KV + kvh) << a.page_shift) + (((job.j0 + t) * KEYS + lane * piece) & ((1 << a.page_shift) - 1));
+#pragma unroll
+                            for (int b = 0; b < L::BANDS; ++b) tma_2d(dst + b * BAND + lane * piece * 128, map, 64 * b, y, bar);
+                        }
+                        if (ahead && (second || !own)) { id = next_id; next_id = page_of(job.j0 + t + 1); }
+                    } else if (lane == 0) {
+                        bar_expect(bar, L::TILE);
+#pragma unroll
+                        for (int b = 0; b < L::BANDS; ++b) tma_3d(dst + b * BAND, map, 64 * b, kvh, it.r.row0 + (job.j0 + t) * KEYS, bar);
+                    }
+                    ++fills;
+                    if (++slot == L::TILES) { slot = 0; ++turn_of; }
                 }
-                step0 += job.tiles;
+                step0 += T;
                 more = it.next(a) && it.start < x1;
             }
             // every copy has landed and every product has let go of its tile before the block goes
@@ -552,12 +547,16 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                     settle(x[0]);
                     settle(x[1]);
                     const unsigned groups = PAGED ? info[(step0 + (u >> 1)) % INFO] >> (4 * (u & 1)) & 15u : 15u;
-                    const bool ragged = k0 + SUB - 1 > first_last || groups != 15u;
-                    const int see = last - k0;                       // the row sees keys 0 .. see of the step
-                    if (ragged) {
+                    if (k0 + SUB - 1 > first_last || groups != 15u) {            // what a row does not see is made -inf
 #pragma unroll
-                        for (int i = 0; i < SUB; ++i)
-                            if (i > see || !(groups >> (i >> 4) & 1)) x[i >> 5][i & 31] = 0xff800000u;
+                        for (int c = 0; c < 2; ++c) {
+                            const int n = last - k0 - 32 * c;        // the row sees keys 0 .. n of the 32
+                            uint32_t seen = n >= 31 ? 0xffffffffu : n < 0 ? 0u : (2u << n) - 1;
+                            if (PAGED) seen &= ((groups >> (2 * c) & 1) ? 0xffffu : 0u) | ((groups >> (2 * c) & 2) ? 0xffff0000u : 0u);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!(seen >> i & 1)) x[c][i] = 0xff800000u;
+                        }
                     }
                     float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -572,7 +571,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                             ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a.err, 209);
                             if (!ok) break;
                             fence_after();
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < HD / 32; ++c) {
                                 uint32_t o[32];
                                 tmem_ld(o_at + 32 * c, o);
@@ -588,32 +587,19 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                     uint64_t sums[2] = {0, 0};
                     const uint64_t scale2 = pair_of(a.scale_log2, a.scale_log2), base2 = pair_of(-base, -base);
                     uint32_t p[32];
-                    if (!ragged) {
 #pragma unroll
-                        for (int i = 0; i < SUB; i += 2) {
-                            const uint64_t e = fma2(pair_of(x[i >> 5][i & 31], x[i >> 5][(i & 31) + 1]), scale2, base2);
-                            float v0, v1;
-                            if ((i >> 1) % CUBIC_OF < CUBIC) {
-                                exp2_cubic(e, v0, v1);
-                            } else {
-                                split(e, v0, v1);
-                                v0 = exp2_approx(v0);
-                                v1 = exp2_approx(v1);
-                            }
-                            sums[(i >> 1) & 1] = add2(sums[(i >> 1) & 1], pair_of(v0, v1));
-                            p[i >> 1] = cvt_bf16x2(v0, v1);
+                    for (int i = 0; i < SUB; i += 2) {
+                        const uint64_t e = fma2(pair_of(x[i >> 5][i & 31], x[i >> 5][(i & 31) + 1]), scale2, base2);
+                        float y0, y1;
+                        if ((i >> 1) % CUBIC_OF < CUBIC) {
+                            exp2_cubic(e, y0, y1);
+                        } else {
+                            split(e, y0, y1);
+                            y0 = exp2_approx(y0);
+                            y1 = exp2_approx(y1);
                         }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < SUB; i += 2) {           // zeros also where scale is 0
-                            const bool gone = !(groups >> (i >> 4) & 1);
-                            float v0 = exp2_approx(fmaf(__uint_as_float(x[i >> 5][i & 31]), a.scale_log2, -base));
-                            float v1 = exp2_approx(fmaf(__uint_as_float(x[i >> 5][(i & 31) + 1]), a.scale_log2, -base));
-                            if (i > see || gone) v0 = 0.f;
-                            if (i + 1 > see || gone) v1 = 0.f;
-                            sums[(i >> 1) & 1] = add2(sums[(i >> 1) & 1], pair_of(v0, v1));
-                            p[i >> 1] = cvt_bf16x2(v0, v1);
-                        }
+                        sums[(i >> 1) & 1] = add2(sums[(i >> 1) & 1], pair_of(y0, y1));
+                        p[i >> 1] = cvt_bf16x2(y0, y1);
                     }
                     tmem_st(s_at, p);
                     float sum0, sum1;
@@ -633,7 +619,9 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                     fence_after();
                 }
                 if (live && (steps || (job.from < job.to && !whole))) {
-                    const float f = whole ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
+                    const bool none = m == -INFINITY;                // the row has seen nothing
+                    if (none) l = 0.f;
+                    const float f = none ? 0.f : whole ? __fdividef(1.0f, l) : 1.f;
                     const size_t slot = ((size_t)w * SLOTS + (job.from > 0 ? 0 : 1)) * ROWS;
                     // Lane 4 i + j takes the j-th 16 bytes of each of the rows 4 i .. 4 i + 3: a store of the warp is eight runs of 64 bytes, where a row
                     // per lane is 32 half sectors (the end of an item took 9000 clocks, its stores in the way of the other warps').
@@ -644,7 +632,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                         if (__shfl_sync(0xffffffffu, token, (lane & ~3) + i) < 0) at[i] = -1;
                     }
                     float bad[2] = {0.f, 0.f};                       // 0 times the sums: not 0 where one is not finite
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < HD / 32; ++c) {
                         uint32_t o[32];
                         if (steps) {
