@@ -58,10 +58,10 @@ int *attention_err_ptr() {
     return addr[dev];
 }
 
-template <int HD, bool PAGED> knnssd_status launch_tensor(attn::Args a, cudaStream_t s) {
+template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, cudaStream_t s) {
     using L = tcattn::Lay<HD>;
     static bool configured[kMaxDevices] = {};
-    const auto kernel = tcattn::tensor_kernel<HD, PAGED>;
+    const auto kernel = tcattn::tensor_kernel<HD, MODE>;
     a.err = attention_err_ptr();
     if (!a.err || !allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
     const int G = a.H / a.KV, most = tcattn::HALF_ROWS;
@@ -70,16 +70,16 @@ template <int HD, bool PAGED> knnssd_status launch_tensor(attn::Args a, cudaStre
     a.nvh = a.KV * a.subs;
     a.tb = most / a.gs;
     a.extra = 384; a.least_run = 512; a.pair_most = 1024;
-    CUtensorMap qm, km, vm;
+    CUtensorMap qm{}, km{}, vm{};
     const cuuint64_t qs[3] = {HD, (cuuint64_t)a.H, (cuuint64_t)a.R}, qst[2] = {HD * 2, (cuuint64_t)a.q_stride * 2};
     const cuuint32_t qb[3] = {64, (cuuint32_t)a.gs, (cuuint32_t)a.tb};
     bool made = bf16_map(&qm, a.q, 3, qs, qst, qb);
-    if (PAGED) {
+    if (MODE == tcattn::TILED) {
         const int page = 1 << a.page_shift;
         const cuuint64_t ks[2] = {HD, (cuuint64_t)a.n_pages * a.KV * page}, kst[1] = {HD * 2};
         const cuuint32_t kb[2] = {64, (cuuint32_t)(page < tcattn::KEYS ? page : tcattn::KEYS)};
         made = made && bf16_map(&km, a.k, 2, ks, kst, kb) && bf16_map(&vm, a.v, 2, ks, kst, kb);
-    } else {
+    } else if (MODE == tcattn::PACKED) {
         const cuuint64_t ks[3] = {HD, (cuuint64_t)a.KV, (cuuint64_t)a.R}, kst[2] = {HD * 2, (cuuint64_t)a.k_stride * 2}, vst[2] = {HD * 2, (cuuint64_t)a.v_stride * 2};
         const cuuint32_t kb[3] = {64, 1, tcattn::KEYS};
         made = made && bf16_map(&km, a.k, 3, ks, kst, kb) && bf16_map(&vm, a.v, 3, ks, vst, kb);
@@ -89,7 +89,7 @@ template <int HD, bool PAGED> knnssd_status launch_tensor(attn::Args a, cudaStre
     Scratch mem(s);
     const size_t slots = (size_t)ctas * attn::SLOTS * tcattn::ROWS;
     if (!mem.get(&a.parts, (size_t)ctas) || !mem.get(&a.ml, slots) || !mem.get(&a.o, slots * HD)) return KNNSSD_ERR_CUDA;
-    launch_chained(kernel, dim3(ctas), dim3(tcattn::NT), L::SMEM, s, a, qm, km, vm);
+    launch_chained(kernel, dim3(ctas), dim3(tcattn::threads_of(MODE == tcattn::COPIED)), L::SMEM, s, a, qm, km, vm);
     launch_chained(attn::merge_kernel<HD, bf16_t, true, tcattn::ROWS>, dim3(ctas - 1, tcattn::ROWS / 8), dim3(256), 0, s, a);
     return launched();
 }
@@ -183,9 +183,13 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
     a.scale_log2 = log2_scale(scale);
     a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-    if ((long long)n_pages * page_size * n_kv_heads > INT_MAX) return KNNSSD_ERR_CAPACITY;
     try {
-        if (dtype == 1) return head_dim == 128 ? launch_tensor<128, true>(a, s) : launch_tensor<64, true>(a, s);
+        if (dtype == 1) {
+            // a coordinate of the TMA has 31 bits
+            if (page_size >= 64 && (long long)n_pages * page_size * n_kv_heads <= INT_MAX)
+                return head_dim == 128 ? launch_tensor<128, tcattn::TILED>(a, s) : launch_tensor<64, tcattn::TILED>(a, s);
+            return head_dim == 128 ? launch_tensor<128, tcattn::COPIED>(a, s) : launch_tensor<64, tcattn::COPIED>(a, s);
+        }
         return head_dim == 128 ? launch_paged_rows<128>(a, cache_dtype, s) : launch_paged_rows<64>(a, cache_dtype, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }
 }
@@ -212,7 +216,7 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if (dtype == 1) {
-            return head_dim == 128 ? launch_tensor<128, false>(a, s) : launch_tensor<64, false>(a, s);
+            return head_dim == 128 ? launch_tensor<128, tcattn::PACKED>(a, s) : launch_tensor<64, tcattn::PACKED>(a, s);
         }
         return head_dim == 128 ? launch_rows<128, float, float, false, 1>(a, s) : launch_rows<64, float, float, false, 1>(a, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }

@@ -3,7 +3,7 @@
 // The mathematics is the rows kernel's.  A block of a launch (one per SM) takes two halves of 128 rows (query heads that share a K/V head times
 // new rows) through the positions, in tiles of 128 and steps of 64:
 //
-//   warp 8       brings q, K and V in by TMA (128-byte swizzle), a ring of tiles ahead of the products
+//   warp 8       brings q, K and V in, a ring of tiles ahead of the products (K and V of pages: three more warps with it)
 //   warps 9, 10  issue the products of a half each: S = q K^T into tensor memory, O += P V with P read from tensor memory and V as the
 //                transposed operand straight from its row-major tile
 //   warps 0 - 3  the softmax of the first half, a row per thread: scores out of tensor memory, exponentials, P back as bf16 over them
@@ -29,7 +29,8 @@ namespace tcattn {
 using namespace attn;
 
 constexpr int KEYS = 128, SUB = 64, HALF_ROWS = 128, ROWS = 256;      // positions of a tile, and of a step of the softmax
-constexpr int SOFT_WARPS = 8, NT = (SOFT_WARPS + 3) * 32, LOAD_WARP = 8, MMA_WARP = 9;
+constexpr int SOFT_WARPS = 8, LOADERS = 4, LOAD_WARP = 8, MMA_WARP = 9;      // pages: the other loaders are the warps behind the products'
+__host__ __device__ constexpr int threads_of(bool copied) { return (SOFT_WARPS + 2 + (copied ? LOADERS : 1)) * 32; }
 constexpr int NCOST = 128;
 constexpr int BAND = KEYS * 128;          // bytes of 64 dimensions of a tile: rows of 128 bytes, swizzled
 constexpr int INFO = 16;                  // steps whose page masks are kept
@@ -47,9 +48,6 @@ template <int HD> struct Lay {
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t b, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(b), "r"(count)); }
 __device__ __forceinline__ void bar_arrive(uint32_t b) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(b) : "memory"); }
-__device__ __forceinline__ void bar_expect(uint32_t b, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(b), "r"(parity) : "memory");
@@ -71,13 +69,25 @@ __device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity, volatile i
 __device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int *quit, int *err, int code) {
     return __all_sync(0xffffffffu, bar_wait(b, parity, quit, err, code));
 }
-__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y)
+// One thread of the warp, which goes through them as a whole (a branch on the lane costs some 100 clocks per copy: its operands are moved to
+// uniform registers one by one); `one` is 1 in that thread and 0 in the others.
+__device__ __forceinline__ uint32_t elect() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one;
+}
+__device__ __forceinline__ void bar_expect_if(uint32_t b, uint32_t bytes, uint32_t one) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(b), "r"(bytes), "r"(one) : "memory");
+}
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar, uint32_t one) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t"
+                 "@p cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}" ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(one)
                  : "memory");
 }
-__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y),
-                 "r"(z)
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar, uint32_t one) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+                 "@p cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n\t}" ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y),
+                 "r"(z), "r"(one)
                  : "memory");
 }
 // Shared-memory operand descriptors, 128-byte swizzle: address / 16 in bits 0 .. 13, leading offset / 16 in 16 .. 29, stride offset / 16 in
@@ -206,6 +216,9 @@ __device__ __forceinline__ void turn4(uint4 (&v)[4], int lane) {
     swap(v[1], v[3], 2);
 }
 
+// Where K and V come from: packed rows; pages by 16-byte copies; pages of 64 positions or more by TMA.
+enum { PACKED = 0, COPIED = 1, TILED = 2 };
+
 // What a run has of an item: n[h] steps of SUB positions from tile j0 on for either half; a half without rows, or whose rows end before, has none.
 struct Job {
     int from, to, j0, n[2], tiles, seen0, tokens;
@@ -279,10 +292,11 @@ __device__ __forceinline__ void mend_row(const Args &a, int b, int seq_row0, int
     if (!whole) a.ml[slot] = make_float2(m, l);
 }
 
-template <int HD, bool PAGED>
-__global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+template <int HD, int MODE>
+__global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(const Args a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                                                         const __grid_constant__ CUtensorMap vmap) {
     using L = Lay<HD>;
+    constexpr bool PAGED = MODE != PACKED;
     extern __shared__ unsigned char raw[];
     __shared__ Costs<NCOST> costs;
     __shared__ uint64_t bars[2 + 2 + 2 * L::TILES + 4 + 4 + 4];        // s_full, p_full and o_full: [half][buffer]
@@ -299,7 +313,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
             bar_init(q_full + 8 * i, 1); bar_init(q_empty + 8 * i, 1);
             for (int b = 0; b < 2; ++b) { bar_init(o_full + 8 * (2 * i + b), 1); bar_init(s_full + 8 * (2 * i + b), 2); bar_init(p_full + 8 * (2 * i + b), 4); }
         }
-        for (int i = 0; i < L::TILES; ++i) { bar_init(kv_full + 8 * i, 1); bar_init(kv_empty + 8 * i, 2); }
+        for (int i = 0; i < L::TILES; ++i) { bar_init(kv_full + 8 * i, MODE == COPIED ? LOADERS * 32 + 1 : 1); bar_init(kv_empty + 8 * i, 2); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
@@ -311,7 +325,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
     sum_costs<true>(a, costs);                                       // has the block's barriers
     fence_after();
     const uint32_t tmem = tmem_base;
-    if (a.clear) clear_tail<bf16_t>(a, HD, blockIdx.x * NT + tid, gridDim.x * NT);
+    if (a.clear) clear_tail<bf16_t>(a, HD, blockIdx.x * blockDim.x + tid, gridDim.x * blockDim.x);
     const long long total = costs.pfx[NCOST];
     const int w = blockIdx.x, W = total > 0 ? workers_of(a, total, gridDim.x) : 0;
     const long long x0 = w < W ? run_start(total, w, W) : 0, x1 = w < W ? run_start(total, w + 1, W) : 0;
@@ -322,17 +336,28 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
         if (tid == 0) note_part<KEYS>(a, it, w, W, total, x0, x1);
         bool ok = true, more = true;
 
-        if (warp == LOAD_WARP) {
+        if (warp == LOAD_WARP || warp >= MMA_WARP + 2) {
             // ---- copies ------------------------------------------------------------------------------------------------
+            // Packed rows come by TMA, one copy for 64 dimensions of a tile.  A tile of pages of 16 positions would be 16 copies, and a copy takes the issuing
+            // warp some 100 clocks: such pages come by 16-byte asynchronous copies of four warps, laid out as the TMA would.  64 single tokens over
+            // pages of 16 / 32 / 64 / 128 positions: by TMA 171 / 131 / 117 / 115 us, by copies 137 / - / - / 133.  What no row of the block sees, and
+            // what has no page, becomes zeros.
+            const int loader = warp == LOAD_WARP ? 0 : warp - MMA_WARP - 1;
+            const uint32_t one = elect();
             unsigned fills = 0, slot = 0, turn_of = 0, qfills[2] = {0, 0}, step0 = 0;      // slot, turn_of: the ring's next tile
-            const int piece = PAGED ? min(1 << a.page_shift, KEYS) : KEYS, pieces = KEYS / piece;
-            int id = -1, next_id = -1;                               // lane i: the page of piece i of the tile, of the one behind it
+            const int piece = MODE == COPIED ? 16 : min(1 << a.page_shift, KEYS), pieces = KEYS / piece;
+            int id = -1, next_id = -1;                               // pages: lane i: the page of piece i of the tile, of the one behind it
             auto page_of = [&](int j) {
                 const int pos = j * KEYS + lane * piece;
                 if (lane >= pieces || pos >= it.kv || (pos >> a.page_shift) >= a.max_pages) return -1;
                 const int p = __ldg(a.table + (size_t)it.b * a.max_pages + (pos >> a.page_shift));
                 return p < a.n_pages ? p : -1;
             };
+            constexpr int CH = HD / 8, PER = 32 / CH, N = 16 / PER;  // 16-byte pieces of a position; positions a copy of the warp; copies for 16
+            const int chunk = lane % CH, sub = lane / CH;
+            uint32_t turned[8 / PER];                                // where the swizzle puts this lane's piece of its positions, modulo 8
+#pragma unroll
+            for (int n = 0; n < 8 / PER; ++n) turned[n] = ((chunk & 7) ^ (n * PER + sub)) << 4;
             while (more && ok) {
                 const Job job(a, it, x0, x1);
                 // tiles in the order of their use (see the products)
@@ -342,16 +367,14 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
 #pragma unroll 1
                 for (int i = 0; i < total_tiles && ok; ++i) {
                     // half i's q before tile i: the first K is on its way while q waits for the products of the item before
-                    if (i < 2 && (i ? job.n[1] : job.n[0]) > 0) {
+                    if (i < 2 && loader == 0 && (i ? job.n[1] : job.n[0]) > 0) {
                         ok = warp_wait(q_empty + 8 * i, (qfills[i] & 1) ^ 1, &quit, a.err, 202);
                         if (!ok) break;
-                        if (lane == 0) {
-                            const int vh = job.paired ? 2 * it.vh + i : it.vh, h0 = vh / a.subs * (a.H / a.KV) + vh % a.subs * a.gs;
-                            const int row = it.r.row0 + it.rb * it.r.tb + (job.paired ? 0 : i * a.tb);
-                            bar_expect(q_full + 8 * i, a.tb * a.gs * HD * 2);
+                        const int vh = job.paired ? 2 * it.vh + i : it.vh, h0 = a.subs == 1 ? vh * a.gs : vh / a.subs * (a.H / a.KV) + vh % a.subs * a.gs;
+                        const int row = it.r.row0 + it.rb * it.r.tb + (job.paired ? 0 : i * a.tb);
+                        bar_expect_if(q_full + 8 * i, a.tb * a.gs * HD * 2, one);
 #pragma unroll
-                            for (int b = 0; b < L::BANDS; ++b) tma_3d(q_tile + i * L::TILE + b * BAND, &qmap, 64 * b, h0, row, q_full + 8 * i);
-                        }
+                        for (int b = 0; b < L::BANDS; ++b) tma_3d(q_tile + i * L::TILE + b * BAND, &qmap, 64 * b, h0, row, q_full + 8 * i, one);
                         ++qfills[i];
                     }
                     bool is_k, second = false;
@@ -372,31 +395,58 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                     if (!ok) break;
                     const uint32_t dst = ring + slot * L::TILE, bar = kv_full + 8 * slot;
                     const int vh = job.paired ? 2 * it.vh + second : it.vh, kvh = a.subs == 1 ? vh : vh / a.subs;
-                    const CUtensorMap *map = is_k ? &kmap : &vmap;
-                    if (PAGED) {
-                        const int page = ahead ? next_id : id;
-                        const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
-                        if (lane == 0) {
-                            if (is_k && !second) {
-                                unsigned groups = 0;
-                                const unsigned each = (1u << (piece / 16)) - 1;
-                                for (int g = 0; g < pieces; ++g)
-                                    if (there >> g & 1) groups |= each << (g * (piece / 16));
-                                info[(step0 + t) % INFO] = groups;
+                    const int page = ahead ? next_id : id;
+                    const unsigned there = PAGED ? __ballot_sync(0xffffffffu, page >= 0) : 0u;
+                    if (PAGED && is_k && !second && lane == 0 && loader == 0) {
+                        unsigned groups = 0;
+                        const unsigned each = (1u << (piece / 16)) - 1;
+                        for (int g = 0; g < pieces; ++g)
+                            if (there >> g & 1) groups |= each << (g * (piece / 16));
+                        info[(step0 + t) % INFO] = groups;
+                    }
+                    if (PAGED && ahead && (second || !own)) { id = next_id; next_id = page_of(job.j0 + t + 1); }
+                    if (MODE == COPIED) {
+                        const unsigned char *pool = static_cast<const unsigned char *>(is_k ? a.k : a.v);
+                        const uint32_t at = dst + (chunk >> 3) * BAND + sub * 128;
+#pragma unroll 2
+                        for (int g = loader; g < KEYS / 16; g += LOADERS) {
+                            const int pg = __shfl_sync(0xffffffffu, page, g), pos = (job.j0 + t) * KEYS + 16 * g;
+                            const int seen = pg >= 0 ? it.kv - pos - sub : 0;       // positions from this lane's first on that count
+                            const unsigned char *src =
+                                pool + ((((size_t)max(pg, 0) * a.KV + kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) + sub) * (HD * 2) + chunk * 16;
+                            const uint32_t to = at + g * 2048;
+                            if (__all_sync(0xffffffffu, seen >= 16)) {
+#pragma unroll
+                                for (int n = 0; n < N; ++n)
+                                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + n * PER * 128 + turned[n % (8 / PER)]), "l"(src + n * PER * (HD * 2)) : "memory");
+                            } else {
+#pragma unroll 1
+                                for (int n = 0; n < N; ++n) {
+                                    const int row = n * PER, size = row < seen ? 16 : 0;
+                                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + row * 128 + (((chunk & 7) ^ ((row + sub) & 7)) << 4)),
+                                                 "l"(size ? src + row * (HD * 2) : pool), "r"(size)
+                                                 : "memory");
+                                }
                             }
-                            bar_expect(bar, __popc(there) * piece * HD * 2);
                         }
-                        __syncwarp();
-                        if (page >= 0) {
-                            const int y = ((page * a.KV + kvh) << a.page_shift) + (((job.j0 + t) * KEYS + lane * piece) & ((1 << a.page_shift) - 1));
+                        // The barrier has an arrival of each lane when its copies so far have landed, and one that hands on the note.
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                        if (loader == 0 && lane == 0) bar_arrive(bar);
+                    } else if (MODE == TILED) {
+                        const CUtensorMap *map = is_k ? &kmap : &vmap;
+                        __syncwarp();                                // behind the note: the arrival that goes with it hands it on
+                        bar_expect_if(bar, __popc(there) * piece * HD * 2, one);
+                        const int y = ((page * a.KV + kvh) << a.page_shift) + (((job.j0 + t) * KEYS + lane * piece) & ((1 << a.page_shift) - 1));
+                        for (int g = 0; g < pieces; ++g) {
+                            const int yg = __shfl_sync(0xffffffffu, y, g);
 #pragma unroll
-                            for (int b = 0; b < L::BANDS; ++b) tma_2d(dst + b * BAND + lane * piece * 128, map, 64 * b, y, bar);
+                            for (int b = 0; b < L::BANDS; ++b) tma_2d(dst + b * BAND + g * piece * 128, map, 64 * b, yg, bar, there >> g & one);
                         }
-                        if (ahead && (second || !own)) { id = next_id; next_id = page_of(job.j0 + t + 1); }
-                    } else if (lane == 0) {
-                        bar_expect(bar, L::TILE);
+                    } else {
+                        const CUtensorMap *map = is_k ? &kmap : &vmap;
+                        bar_expect_if(bar, L::TILE, one);
 #pragma unroll
-                        for (int b = 0; b < L::BANDS; ++b) tma_3d(dst + b * BAND, map, 64 * b, kvh, it.r.row0 + (job.j0 + t) * KEYS, bar);
+                        for (int b = 0; b < L::BANDS; ++b) tma_3d(dst + b * BAND, map, 64 * b, kvh, it.r.row0 + (job.j0 + t) * KEYS, bar, one);
                     }
                     ++fills;
                     if (++slot == L::TILES) { slot = 0; ++turn_of; }
@@ -404,11 +454,12 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                 step0 += T;
                 more = it.next(a) && it.start < x1;
             }
+            if (MODE == COPIED) asm volatile("cp.async.wait_all;" ::: "memory");
             // every copy has landed and every product has let go of its tile before the block goes
-            for (unsigned i = fills > L::TILES ? fills - L::TILES : 0; i < fills; ++i) {
+            for (unsigned i = loader ? fills : fills > L::TILES ? fills - L::TILES : 0; i < fills; ++i) {
                 const unsigned slot = i % L::TILES, parity = i / L::TILES & 1;
                 if (ok) ok = warp_wait(kv_empty + 8 * slot, parity, &quit, a.err, 203);
-                if (!ok)
+                if (MODE != COPIED && !ok)
                     for (unsigned spins = 0; spins < WAIT_LIMIT && !bar_try(kv_full + 8 * slot, parity); ++spins) {}
             }
             for (int h = 0; h < 2; ++h)
@@ -430,7 +481,10 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
             // Either half goes through every tile of the ring, waits for it and lets it go, whether it has a use for it or not: a half that left the
             // other's tiles out could be a turn of the ring ahead, where a barrier's parity no longer tells one phase from the next.
             unsigned walked = 0;
-            auto there = [&]() { if (ok) ok = warp_wait(kv_full + 8 * slot, phase, &quit, a.err, 205); };
+            auto there = [&]() {
+                if (ok) ok = warp_wait(kv_full + 8 * slot, phase, &quit, a.err, 205);
+                if (MODE == COPIED) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // ordinary copies before the products' reads
+            };
             auto onward = [&]() {
                 ++walked;
                 if (++slot == L::TILES) { slot = 0; phase ^= 1; }
@@ -449,7 +503,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                 onward();
             };
             // What lies behind the last position that the block sees, and what has no page, must be zero in V: its p is 0, and 0 times what happens
-            // to lie there need not be.  (Where the halves share the tile both do it.)
+            // to lie there need not be.  (Where the halves share the tile both do it; copies of 16 bytes bring the zeros.)
             auto clean = [&](uint32_t v, int valid, unsigned groups) {
                 for (int i = lane; i < KEYS * 8; i += 32) {
                     const int row = i >> 3;
@@ -493,8 +547,8 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                             if (own) pass(h ? (t == T - 1 ? 1 : 2) : (t == 0 ? 1 : 2));
                             take(v, v_bar);
                             const int valid = it.kv - (job.j0 + t) * KEYS;
-                            const unsigned groups = PAGED ? info[(step0 + t) % INFO] : 0xffu;
-                            if (ok && (valid < KEYS || groups != 0xffu)) clean(v, valid, groups);
+                            const unsigned groups = MODE == TILED ? info[(step0 + t) % INFO] : 0xffu;
+                            if (MODE != COPIED && ok && (valid < KEYS || groups != 0xffu)) clean(v, valid, groups);
                         }
                         if (ok) ok = warp_wait(my_p + 8 * vbuf, p_phase, &quit, a.err, 206);
                         if (!ok) break;
@@ -507,7 +561,7 @@ __global__ void __launch_bounds__(NT, 1) tensor_kernel(const Args a, const __gri
                     }
                 }
                 pass((own ? 4 : 2) * T - walked);
-                step0 += job.tiles;
+                step0 += T;
                 more = it.next(a) && it.start < x1;
             }
         } else {
