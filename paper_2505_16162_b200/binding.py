@@ -268,16 +268,17 @@ def knnssd_cosine_top1_static(query: torch.Tensor, anchors: torch.Tensor):
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _i32(t: torch.Tensor, shape, what: str) -> int:
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous CUDA int32 tensor of shape {tuple(shape)}")
+# (These calls take a few microseconds of the GPU's time, so their checks are kept cheap: sizes by numel, devices by index.)
+def _i32(t: torch.Tensor, n: int, dev: int, what: str) -> int:
+    if t.dtype is not torch.int32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor of {n} values on the call's CUDA device")
     return t.data_ptr()
 
 
-def _rows(t: torch.Tensor, what: str) -> int:
-    """Address of [rows][heads][head_dim] values whose rows are dense; the rows may be any distance apart."""
-    if t.dim() != 3 or not t.is_cuda or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError(f"{what} must be a CUDA tensor [rows][heads][head_dim] whose heads are contiguous")
+def _rows(t: torch.Tensor, dev: int, what: str) -> int:
+    """Address of [rows][heads][head_dim] values whose heads are contiguous; the rows may be any distance apart."""
+    if t.dim() != 3 or t.get_device() != dev or t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] > 1):
+        raise ValueError(f"{what} must be a tensor [rows][heads][head_dim] on the call's CUDA device whose heads are contiguous")
     return t.data_ptr()
 
 
@@ -285,32 +286,34 @@ def _row_stride(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
-def _pages(k: torch.Tensor, v: torch.Tensor):
-    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not (k.is_cuda and v.is_cuda and k.is_contiguous() and v.is_contiguous()):
-        raise ValueError("k_pages and v_pages must be contiguous CUDA tensors [n_pages][n_kv_heads][page_size][head_dim] of one type")
-    return k.shape
+def _pages(k: torch.Tensor, v: torch.Tensor, dev: int):
+    shape = k.shape
+    if len(shape) != 4 or v.shape != shape or k.dtype is not v.dtype or k.get_device() != dev or v.get_device() != dev or not (k.is_contiguous() and v.is_contiguous()):
+        raise ValueError("k_pages and v_pages must be contiguous tensors [n_pages][n_kv_heads][page_size][head_dim] of one type on the call's CUDA device")
+    return shape
 
 
 def _type(t: torch.Tensor, what: str) -> int:
-    if t.dtype not in _DTYPES:
+    d = _DTYPES.get(t.dtype)
+    if d is None:
         raise ValueError(f"{what} must be float32 or bfloat16, got {t.dtype}")
-    return _DTYPES[t.dtype]
+    return d
 
 
-def _same_device(*tensors: torch.Tensor):
-    first = tensors[0].device
-    for t in tensors:
-        if t.device != first:
-            raise ValueError("all tensors of a call must be on one device")
+def _device(t: torch.Tensor) -> int:
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("expected tensors on a CUDA device")
+    return dev
 
 
-def _call(fn, name: str, device: torch.device, *args):
-    """fn(*args, stream) on `device`'s current stream."""
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+def _call(fn, name: str, dev: int, *args):
+    """fn(*args, stream) on the current stream of CUDA device `dev`."""
+    if torch.cuda.current_device() == dev:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         raise KnnssdError(rc, name)
 
@@ -321,14 +324,15 @@ def knnssd_page_tables(lens: torch.Tensor, fresh: torch.Tensor, owned: torch.Ten
     """The pages of one step and the slots of its rows, on the GPU; all tensors int32, contiguous.  lens, fresh [B] in; owned [B], table
     [B][max_pages], free_pages [n_pages], free_count [1] in and out; row_start [B + 1], row_request / row_pos / row_slot [max_rows], info [4]
     (rows, pages taken, pages given back, what is wrong) out.  See the header for the order pages go in."""
-    if lens.dim() != 1 or table.dim() != 2 or free_pages.dim() != 1 or row_pos.dim() != 1:
-        raise ValueError("lens, free_pages and the rows' maps have one dimension, table two")
-    B, n_pages, rows, max_pages = lens.shape[0], free_pages.shape[0], row_pos.shape[0], table.shape[1]
-    _same_device(lens, fresh, owned, table, free_pages, free_count, row_start, row_request, row_pos, row_slot, info)
-    _call(_lib.knnssd_page_tables, "knnssd_page_tables", lens.device, _i32(lens, (B,), "lens"), _i32(fresh, (B,), "fresh"), B, page_size, max_pages, n_pages,
-          _i32(owned, (B,), "owned"), _i32(table, (B, max_pages), "table"), _i32(free_pages, (n_pages,), "free_pages"), _i32(free_count, (1,), "free_count"), rows,
-          _i32(row_start, (B + 1,), "row_start"), _i32(row_request, (rows,), "row_request"), _i32(row_pos, (rows,), "row_pos"),
-          _i32(row_slot, (rows,), "row_slot"), _i32(info, (4,), "info"))
+    dev = _device(lens)
+    if lens.dim() != 1 or table.dim() != 2 or table.shape[0] != lens.shape[0]:
+        raise ValueError("lens must be [requests], table [requests][max_pages]")
+    B, max_pages = table.shape
+    n_pages, rows = free_pages.numel(), row_pos.numel()
+    _call(_lib.knnssd_page_tables, "knnssd_page_tables", dev, _i32(lens, B, dev, "lens"), _i32(fresh, B, dev, "fresh"), B, page_size, max_pages, n_pages,
+          _i32(owned, B, dev, "owned"), _i32(table, B * max_pages, dev, "table"), _i32(free_pages, n_pages, dev, "free_pages"),
+          _i32(free_count, 1, dev, "free_count"), rows, _i32(row_start, B + 1, dev, "row_start"), _i32(row_request, rows, dev, "row_request"),
+          _i32(row_pos, rows, dev, "row_pos"), _i32(row_slot, rows, dev, "row_slot"), _i32(info, 4, dev, "info"))
 
 
 def rotary_table(n_positions: int, head_dim: int, theta: float, device="cuda") -> torch.Tensor:
@@ -342,29 +346,30 @@ def knnssd_rotary_store(qkv: torch.Tensor, cos_sin: torch.Tensor, row_pos: torch
                         v_pages: torch.Tensor, q: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotates the q and k heads of the rows of qkv [rows][(n_heads + 2 n_kv_heads) head_dim] by their positions, puts K and V into their
     slots and returns q [rows][n_heads][head_dim] in qkv's type."""
-    n_pages, kv, page, hd = _pages(k_pages, v_pages)
+    dev = _device(qkv)
+    n_pages, kv, page, hd = _pages(k_pages, v_pages, dev)
     dtype, cache = _type(qkv, "qkv"), _type(k_pages, "k_pages")
-    if qkv.dim() != 2 or not qkv.is_cuda or qkv.stride(1) != 1 or qkv.shape[1] % hd != 0 or qkv.shape[1] // hd <= 2 * kv:
-        raise ValueError("qkv must be a CUDA tensor [rows][(n_heads + 2 n_kv_heads) head_dim] with dense rows")
-    rows, heads = qkv.shape[0], qkv.shape[1] // hd - 2 * kv
-    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 3 or cos_sin.shape[1:] != (hd // 2, 2) or not cos_sin.is_cuda or not cos_sin.is_contiguous():
-        raise ValueError("cos_sin must be a contiguous CUDA float32 tensor [positions][head_dim / 2][2]")
+    if qkv.dim() != 2 or qkv.stride(1) != 1 or qkv.shape[1] % hd != 0 or qkv.shape[1] // hd <= 2 * kv:
+        raise ValueError("qkv must be a tensor [rows][(n_heads + 2 n_kv_heads) head_dim] with dense rows")
+    rows, width = qkv.shape
+    heads = width // hd - 2 * kv
+    if cos_sin.dtype is not torch.float32 or cos_sin.dim() != 3 or cos_sin.shape[1] != hd // 2 or cos_sin.shape[2] != 2 or cos_sin.get_device() != dev or not cos_sin.is_contiguous():
+        raise ValueError("cos_sin must be a contiguous float32 tensor [positions][head_dim / 2][2] on the call's CUDA device")
     if q is None:
         q = torch.empty((rows, heads, hd), dtype=qkv.dtype, device=qkv.device)
-    elif q.shape != (rows, heads, hd) or q.dtype != qkv.dtype or not q.is_cuda or not q.is_contiguous():
-        raise ValueError("q must be a contiguous CUDA tensor [rows][n_heads][head_dim] of qkv's type")
-    _same_device(qkv, cos_sin, row_pos, row_slot, k_pages, v_pages, q)
-    _call(_lib.knnssd_rotary_store, "knnssd_rotary_store", qkv.device, qkv.data_ptr(), dtype, rows, qkv.stride(0) if rows > 1 else qkv.shape[1], heads, kv, hd,
-          cos_sin.data_ptr(), cos_sin.shape[0], _i32(row_pos, (rows,), "row_pos"), _i32(row_slot, (rows,), "row_slot"), page, n_pages, q.data_ptr(),
+    elif q.shape != (rows, heads, hd) or q.dtype is not qkv.dtype or q.get_device() != dev or not q.is_contiguous():
+        raise ValueError("q must be a contiguous tensor [rows][n_heads][head_dim] of qkv's type on its device")
+    _call(_lib.knnssd_rotary_store, "knnssd_rotary_store", dev, qkv.data_ptr(), dtype, rows, qkv.stride(0) if rows > 1 else width, heads, kv, hd,
+          cos_sin.data_ptr(), cos_sin.shape[0], _i32(row_pos, rows, dev, "row_pos"), _i32(row_slot, rows, dev, "row_slot"), page, n_pages, q.data_ptr(),
           k_pages.data_ptr(), v_pages.data_ptr(), cache)
     return q
 
 
-def _attention_out(q: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
+def _attention_out(q: torch.Tensor, dev: int, out: Optional[torch.Tensor]) -> torch.Tensor:
     if out is None:
         return torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if out.shape != q.shape or out.dtype != q.dtype or not out.is_cuda or not out.is_contiguous():
-        raise ValueError("out must be a contiguous CUDA tensor of q's shape and type")
+    if out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != dev or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape and type on its device")
     return out
 
 
@@ -374,17 +379,17 @@ def knnssd_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
     """Attention of the new rows q [rows][n_heads][head_dim] over the requests' pages: row row_start[b] + i sees positions 0 .. lens[b] + i.
     table [B][max_pages], lens [B], row_start [B + 1] int32.  max_fresh: the most rows of a request in this call, if known.  scale defaults to
     head_dim ** -0.5."""
-    n_pages, kv, page, hd = _pages(k_pages, v_pages)
+    dev = _device(q)
+    n_pages, kv, page, hd = _pages(k_pages, v_pages, dev)
     dtype, cache = _type(q, "q"), _type(k_pages, "k_pages")
-    qp = _rows(q, "q")
-    if q.shape[2] != hd or table.dim() != 2:
+    qp = _rows(q, dev, "q")
+    rows, heads, width = q.shape
+    if width != hd or table.dim() != 2:
         raise ValueError("q's head_dim must be the pages', and table must be [requests][max_pages]")
-    rows, heads, _ = q.shape
     B, max_pages = table.shape
-    out = _attention_out(q, out)
-    _same_device(q, k_pages, v_pages, table, lens, row_start, out)
-    _call(_lib.knnssd_paged_attention, "knnssd_paged_attention", q.device, qp, dtype, rows, _row_stride(q), heads, kv, hd, k_pages.data_ptr(), v_pages.data_ptr(),
-          cache, page, n_pages, _i32(table, (B, max_pages), "table"), max_pages, _i32(lens, (B,), "lens"), _i32(row_start, (B + 1,), "row_start"), B, max_fresh,
+    out = _attention_out(q, dev, out)
+    _call(_lib.knnssd_paged_attention, "knnssd_paged_attention", dev, qp, dtype, rows, _row_stride(q), heads, kv, hd, k_pages.data_ptr(), v_pages.data_ptr(),
+          cache, page, n_pages, _i32(table, B * max_pages, dev, "table"), max_pages, _i32(lens, B, dev, "lens"), _i32(row_start, B + 1, dev, "row_start"), B, max_fresh,
           hd ** -0.5 if scale is None else scale, out.data_ptr())
     return out
 
@@ -393,16 +398,16 @@ def knnssd_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, r
                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Causal attention over packed prompts: q [rows][n_heads][head_dim], k, v [rows][n_kv_heads][head_dim] of one type, rows any distance
     apart; prompt b is the rows row_start[b] .. row_start[b + 1] - 1.  scale defaults to head_dim ** -0.5."""
+    dev = _device(q)
     dtype = _type(q, "q")
-    qp, kp, vp = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    qp, kp, vp = _rows(q, dev, "q"), _rows(k, dev, "k"), _rows(v, dev, "v")
     rows, heads, hd = q.shape
-    if k.shape != v.shape or k.dtype != q.dtype or v.dtype != q.dtype or k.shape[0] != rows or k.shape[2] != hd or row_start.dim() != 1 or row_start.shape[0] < 2:
+    if k.shape != v.shape or k.dtype is not q.dtype or v.dtype is not q.dtype or k.shape[0] != rows or k.shape[2] != hd or row_start.dim() != 1 or row_start.shape[0] < 2:
         raise ValueError("k and v must be [rows][n_kv_heads][head_dim] of q's type, row_start [prompts + 1]")
     B = row_start.shape[0] - 1
-    out = _attention_out(q, out)
-    _same_device(q, k, v, row_start, out)
-    _call(_lib.knnssd_packed_attention, "knnssd_packed_attention", q.device, qp, kp, vp, dtype, rows, _row_stride(q), _row_stride(k), _row_stride(v), heads,
-          k.shape[1], hd, _i32(row_start, (B + 1,), "row_start"), B, hd ** -0.5 if scale is None else scale, out.data_ptr())
+    out = _attention_out(q, dev, out)
+    _call(_lib.knnssd_packed_attention, "knnssd_packed_attention", dev, qp, kp, vp, dtype, rows, _row_stride(q), _row_stride(k), _row_stride(v), heads,
+          k.shape[1], hd, _i32(row_start, B + 1, dev, "row_start"), B, hd ** -0.5 if scale is None else scale, out.data_ptr())
     return out
 
 

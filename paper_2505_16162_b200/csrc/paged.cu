@@ -28,6 +28,17 @@ template <typename K> bool allow_smem(K kernel, int bytes, bool (&done)[kMaxDevi
     return done[dev];
 }
 
+// The parts of items that `workers` of a launch may leave, `rows` rows each: one piece of scratch.
+bool get_parts(Scratch &mem, attn::Args &a, int workers, int rows, int hd) {
+    const size_t slots = (size_t)workers * attn::SLOTS * rows, o_bytes = slots * hd * sizeof(float), ml_bytes = slots * sizeof(float2);
+    unsigned char *p = nullptr;
+    if (!mem.get(&p, o_bytes + ml_bytes + (size_t)workers * sizeof(attn::Part))) return false;
+    a.o = reinterpret_cast<float *>(p);
+    a.ml = reinterpret_cast<float2 *>(p + o_bytes);
+    a.parts = reinterpret_cast<attn::Part *>(p + o_bytes + ml_bytes);
+    return true;
+}
+
 template <int HD, typename QT, typename KT, bool PAGED, int MB> knnssd_status launch_rows(attn::Args a, cudaStream_t s) {
     using Rg = rowattn::Ring<HD, KT>;
     static bool configured[kMaxDevices] = {};
@@ -40,8 +51,7 @@ template <int HD, typename QT, typename KT, bool PAGED, int MB> knnssd_status la
     a.tb = most / a.gs;
     const int ctas = sm_count(), warps = ctas * Rg::WARPS;
     Scratch mem(s);
-    const size_t slots = (size_t)warps * attn::SLOTS * most;
-    if (!mem.get(&a.parts, (size_t)warps) || !mem.get(&a.ml, slots) || !mem.get(&a.o, slots * HD)) return KNNSSD_ERR_CUDA;
+    if (!get_parts(mem, a, warps, most, HD)) return KNNSSD_ERR_CUDA;
     launch_chained(kernel, dim3(ctas), dim3(Rg::WARPS * 32), Rg::SMEM, s, a);
     launch_chained(attn::merge_kernel<HD, QT, false, 16 * MB>, dim3(warps - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
     return launched();
@@ -87,8 +97,7 @@ template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, cudaStream
     if (!made) return KNNSSD_ERR_CUDA;
     const int ctas = sm_count();
     Scratch mem(s);
-    const size_t slots = (size_t)ctas * attn::SLOTS * tcattn::ROWS;
-    if (!mem.get(&a.parts, (size_t)ctas) || !mem.get(&a.ml, slots) || !mem.get(&a.o, slots * HD)) return KNNSSD_ERR_CUDA;
+    if (!get_parts(mem, a, ctas, tcattn::ROWS, HD)) return KNNSSD_ERR_CUDA;
     launch_chained(kernel, dim3(ctas), dim3(tcattn::threads_of(MODE == tcattn::COPIED)), L::SMEM, s, a, qm, km, vm);
     launch_chained(attn::merge_kernel<HD, bf16_t, true, tcattn::ROWS>, dim3(ctas - 1, tcattn::ROWS / 8), dim3(256), 0, s, a);
     return launched();
