@@ -45,7 +45,7 @@ struct Part { long long start; int first, kv, from, to, row0, rows, vh, paired; 
 // where a request has no more rows than one of them and few positions, the halves take two heads instead (paired).
 struct Request { int n, held, row0, tb, nvh; bool paired; long long cost; };
 
-template <bool HALVES> __device__ __forceinline__ Request request_of(const Args &a, int b) {
+template <bool HALVES> __device__ __forceinline__ Request request_here(const Args &a, int b) {
     Request r;
     const int r0 = min(max(a.row_start[b], 0), a.R), r1 = min(max(a.row_start[b + 1], 0), a.R);
     r.n = max(r1 - r0, 0);
@@ -57,6 +57,13 @@ template <bool HALVES> __device__ __forceinline__ Request request_of(const Args 
     const long long whole = r.n / r.tb, left = r.n % r.tb, each = (long long)r.held + a.extra;
     r.cost = (whole * each + r.tb * (whole * (whole + 1) / 2) + (left ? each + r.n : 0)) * r.nvh;
     return r;
+}
+
+// The rows kernel keeps its code small (its warps run apart, each through all of it), the tensor kernel its registers.
+static __device__ __noinline__ Request request_apart(const Args &a, int b) { return request_here<false>(a, b); }
+template <bool HALVES> __device__ __forceinline__ Request request_of(const Args &a, int b) {
+    if constexpr (HALVES) return request_here<true>(a, b);
+    else return request_apart(a, b);
 }
 
 // An item and where it begins among all items' positions.

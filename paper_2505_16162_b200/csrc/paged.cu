@@ -39,12 +39,12 @@ bool get_parts(Scratch &mem, attn::Args &a, int workers, int rows, int hd) {
     return true;
 }
 
-template <int HD, typename QT, typename KT, bool PAGED, int MB> knnssd_status launch_rows(attn::Args a, cudaStream_t s) {
+template <int HD, typename KT, bool PAGED> knnssd_status launch_rows(attn::Args a, cudaStream_t s) {
     using Rg = rowattn::Ring<HD, KT>;
     static bool configured[kMaxDevices] = {};
-    const auto kernel = rowattn::rows_kernel<HD, QT, KT, PAGED, MB>;
+    const auto kernel = rowattn::rows_kernel<HD, KT, PAGED>;
     if (!allow_smem(kernel, Rg::SMEM, configured)) return KNNSSD_ERR_CUDA;
-    const int G = a.H / a.KV, most = 16 * MB;
+    const int G = a.H / a.KV, most = 16;
     a.gs = (G + (G + most - 1) / most - 1) / ((G + most - 1) / most);
     a.subs = (G + a.gs - 1) / a.gs;
     a.nvh = a.KV * a.subs;
@@ -53,7 +53,7 @@ template <int HD, typename QT, typename KT, bool PAGED, int MB> knnssd_status la
     Scratch mem(s);
     if (!get_parts(mem, a, warps, most, HD)) return KNNSSD_ERR_CUDA;
     launch_chained(kernel, dim3(ctas), dim3(Rg::WARPS * 32), Rg::SMEM, s, a);
-    launch_chained(attn::merge_kernel<HD, QT, false, 16 * MB>, dim3(warps - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
+    launch_chained(attn::merge_kernel<HD, float, false, 16>, dim3(warps - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
     return launched();
 }
 
@@ -104,7 +104,7 @@ template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, cudaStream
 }
 
 template <int HD> knnssd_status launch_paged_rows(const attn::Args &a, int cache_dtype, cudaStream_t s) {
-    return cache_dtype == 0 ? launch_rows<HD, float, float, true, 1>(a, s) : launch_rows<HD, float, bf16_t, true, 1>(a, s);
+    return cache_dtype == 0 ? launch_rows<HD, float, true>(a, s) : launch_rows<HD, bf16_t, true>(a, s);
 }
 
 template <int HD> void launch_rotary(const pages::RotaryArgs &a, int dtype, int cache_dtype, cudaStream_t s) {
@@ -227,7 +227,7 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
         if (dtype == 1) {
             return head_dim == 128 ? launch_tensor<128, tcattn::PACKED>(a, s) : launch_tensor<64, tcattn::PACKED>(a, s);
         }
-        return head_dim == 128 ? launch_rows<128, float, float, false, 1>(a, s) : launch_rows<64, float, float, false, 1>(a, s);
+        return head_dim == 128 ? launch_rows<128, float, false>(a, s) : launch_rows<64, float, false>(a, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }
 }
 

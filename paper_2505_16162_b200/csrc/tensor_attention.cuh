@@ -293,7 +293,7 @@ __device__ __forceinline__ void mend_row(const Args &a, int b, int seq_row0, int
 }
 
 template <int HD, int MODE>
-__global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(const Args a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+__global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                                                         const __grid_constant__ CUtensorMap vmap) {
     using L = Lay<HD>;
     constexpr bool PAGED = MODE != PACKED;
