@@ -185,34 +185,38 @@ __device__ __forceinline__ float exp2_approx(float x) {
 }
 
 // Items in parts.  Block (w, j) does eight rows, j 8 .., of the item that worker w's run is the first to begin within: the part of worker w - 1
-// and those behind it until the item's end, in their order.  A warp per row: its lanes share the parts' (m, l) out, then hd / 32
-// dimensions each.
+// and those behind it until the item's end, in their order.  Of few rows each has several of the block's eight warps, which share its parts out;
+// a warp's lanes share the parts' (m, l) out, then hd / 32 dimensions each.
 template <int HD, typename QT, bool HALVES, int ROWS>
 __global__ void __launch_bounds__(256) merge_kernel(const Args a) {
+    constexpr int D = HD / 32;
+    __shared__ float2 ml_of[8];
+    __shared__ float o_of[8][HD];
     chain_wait();
-    const int w = blockIdx.x + 1, lane = threadIdx.x & 31;
+    const int w = blockIdx.x + 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const Part p = a.parts[w];
     if (!p.first) return;
-    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
-    int token, head;
-    place_of<HALVES, ROWS>(a, p.rows, p.vh, p.paired, r, token, head);
-    if (token < 0) return;
+    const int rows = HALVES ? ROWS : min(ROWS, p.rows * a.gs), here = min(8, rows - (int)blockIdx.y * 8);
+    if (here <= 0) return;
+    const int share = here > 4 ? 1 : here > 2 ? 2 : here > 1 ? 4 : 8;            // warps a row
+    const int r = blockIdx.y * 8 + warp / share, mine = warp % share;
+    int token = -1, head = 0;
+    if (warp / share < here) place_of<HALVES, ROWS>(a, p.rows, p.vh, p.paired, r, token, head);
     // part i: of run w - 1 + i, as long as the runs begin in this item
     auto slot = [&](int i) { return ((size_t)(w - 1 + i) * SLOTS + (i == 0 ? 1 : 0)) * ROWS + r; };
     const int most = gridDim.x + 2 - w;
-    constexpr int D = HD / 32;
     float o[D], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < D; ++i) o[i] = 0.f;
-    for (int i0 = 0;; i0 += 32) {
+    for (int i0 = mine * 32; token >= 0; i0 += 32 * share) {
         const int i = i0 + lane;
-        bool mine = i < most, there = mine;                          // there: not cut away
-        if (mine && i > 0) {
+        bool its = i < most, there = its;                            // there: not cut away
+        if (its && i > 0) {
             const Part *q = a.parts + w - 1 + i;
-            mine = q->start == p.start;
-            there = mine && q->from < q->to;
+            its = q->start == p.start;
+            there = its && q->from < q->to;
         }
-        const unsigned all = __ballot_sync(0xffffffffu, mine);
+        const unsigned all = __ballot_sync(0xffffffffu, its);
         const int n = all == 0xffffffffu ? 32 : __ffs(~all) - 1;      // lanes up to the first that is not of the item
         there = there && lane < n;
         const float2 v = there ? a.ml[slot(i)] : make_float2(-INFINITY, 0.f);
@@ -244,6 +248,22 @@ __global__ void __launch_bounds__(256) merge_kernel(const Args a) {
         }
         if (n < 32) break;
     }
+    if (share > 1) {                                                 // the row's warps, in their order
+        if (lane == 0) ml_of[warp] = make_float2(m, l);
+#pragma unroll
+        for (int j = 0; j < D; ++j) o_of[warp][lane * D + j] = o[j];
+        __syncthreads();
+        if (mine > 0) return;
+        for (int u = 1; u < share; ++u) {
+            const float2 v = ml_of[warp + u];
+            const float mn = fmaxf(m, v.x), base = mn == -INFINITY ? 0.f : mn, f = exp2_approx(v.x - base), old = exp2_approx(m - base);
+            m = mn;
+            l = l * old + v.y * f;
+#pragma unroll
+            for (int j = 0; j < D; ++j) o[j] = o[j] * old + f * o_of[warp + u][lane * D + j];
+        }
+    }
+    if (token < 0) return;
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     QT *d = static_cast<QT *>(a.out) + ((size_t)(p.row0 + token) * a.H + head) * HD + lane * D;
 #pragma unroll

@@ -211,31 +211,36 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
 #pragma unroll
                         for (int i = 0; i < 4; ++i) sp[n][u][i] = 0.f;
 #pragma unroll
-                for (int c = 0; c < HD / 32; ++c)
+                for (int c = 0; c < HD / 32; ++c) {                  // products that follow one another go to different sums
+                    if constexpr (NK == 1) {
+                        uint4 k4[2];
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const int pos = 8 * n + g;
-                        if constexpr (NK == 1) {
-                            const uint4 k4 = lds16(kb + pos * Rg::ROW + Rg::kswz(pos, 4 * c + t) * 16);
+                        for (int n = 0; n < 2; ++n) k4[n] = lds16(kb + (8 * n + g) * Rg::ROW + Rg::kswz(g, 4 * c + t) * 16);
 #pragma unroll
-                            for (int i = NQ - 1; i >= 0; --i) {
-                                mma(sp[n][i ? 2 : 0], qf[2 * c][i], k4.x, k4.y);
-                                mma(sp[n][i ? 2 : 1], qf[2 * c + 1][i], k4.z, k4.w);
+                        for (int i = NQ - 1; i >= 0; --i)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                                for (int n = 0; n < 2; ++n) mma(sp[n][i ? 2 : e], qf[2 * c + e][i], e ? k4[n].z : k4[n].x, e ? k4[n].w : k4[n].y);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            uint32_t b0[2][NK], b1[2][NK];
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) {
+                                const uint4 k4 = lds16(kb + (8 * n + g) * Rg::ROW + Rg::kswz(g, 8 * c + 4 * e + t) * 16);
+                                terms_of<NK>(__uint_as_float(k4.x), __uint_as_float(k4.y), b0[n]);
+                                terms_of<NK>(__uint_as_float(k4.z), __uint_as_float(k4.w), b1[n]);
                             }
-                        } else {
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const uint4 k4 = lds16(kb + pos * Rg::ROW + Rg::kswz(pos, 8 * c + 4 * e + t) * 16);
-                                uint32_t b0[NK], b1[NK];
-                                terms_of<NK>(__uint_as_float(k4.x), __uint_as_float(k4.y), b0);
-                                terms_of<NK>(__uint_as_float(k4.z), __uint_as_float(k4.w), b1);
+                            for (int i = NQ - 1; i >= 0; --i)
 #pragma unroll
-                                for (int i = NQ - 1; i >= 0; --i)
+                                for (int j = NK - 1 - i; j >= 0; --j)
 #pragma unroll
-                                    for (int j = NK - 1 - i; j >= 0; --j) mma(sp[n][i + j ? 2 : e], qf[2 * c + e][i], b0[j], b1[j]);
-                            }
+                                    for (int n = 0; n < 2; ++n) mma(sp[n][i + j ? 2 : e], qf[2 * c + e][i], b0[n][j], b1[n][j]);
                         }
                     }
+                }
                 const bool ragged = hole || p + TP - 1 > seen0;      // some row does not see all of these positions
                 uint32_t pf[NQ][4];
 #pragma unroll
@@ -288,14 +293,18 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                 }
                 // o[n][2 e + i] is dimension col(n, i) of row 8 e + g
                 auto col = [&](int n, int i) { return NK == 1 ? 8 * n + 2 * t + i : 32 * (n >> 2) + 4 * (2 * t + i) + (n & 3); };
-                auto products = [&](int n, const uint32_t (&b0)[NK], const uint32_t (&b1)[NK]) {
-                    float d[4] = {0.f, 0.f, 0.f, 0.f};
+                auto products = [&](int n, const uint32_t (&b0)[2][NK], const uint32_t (&b1)[2][NK]) {       // of 16 dimensions: tiles n and n + 1
+                    float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
                     for (int i = NQ - 1; i >= 0; --i)
 #pragma unroll
-                        for (int j = NK == 1 ? 0 : NK - 1 - i; j >= 0; --j) mma(d, pf[i], b0[j], b1[j]);
+                        for (int j = NK == 1 ? 0 : NK - 1 - i; j >= 0; --j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[n][i] += d[i];
+                            for (int u = 0; u < 2; ++u) mma(d[u], pf[i], b0[u][j], b1[u][j]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[n + u][i] += d[u][i];
                 };
                 if (odd) {                                           // position by position, into the rows that see it
 #pragma unroll 1
@@ -337,9 +346,8 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                         uint32_t r[4];
                         const int pos = (lane & 7) + ((lane >> 3) & 1) * 8;
                         ldsm4t(vb + pos * Rg::ROW + Rg::vswz(pos, 2 * n2 + (lane >> 4)) * 16, r);
-                        const uint32_t b0[1] = {r[0]}, b1[1] = {r[1]}, c0[1] = {r[2]}, c1[1] = {r[3]};
+                        const uint32_t b0[2][1] = {{r[0]}, {r[2]}}, b1[2][1] = {{r[1]}, {r[3]}};
                         products(2 * n2, b0, b1);
-                        products(2 * n2 + 1, c0, c1);
                     }
                 } else {
 #pragma unroll
@@ -353,10 +361,13 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                         const uint32_t u[4][4] = {{v4[0].x, v4[0].y, v4[0].z, v4[0].w}, {v4[1].x, v4[1].y, v4[1].z, v4[1].w},
                                                   {v4[2].x, v4[2].y, v4[2].z, v4[2].w}, {v4[3].x, v4[3].y, v4[3].z, v4[3].w}};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t b0[NK], b1[NK];
-                            terms_of<NK>(__uint_as_float(u[0][i]), __uint_as_float(u[1][i]), b0);
-                            terms_of<NK>(__uint_as_float(u[2][i]), __uint_as_float(u[3][i]), b1);
+                        for (int i = 0; i < 4; i += 2) {
+                            uint32_t b0[2][NK], b1[2][NK];
+#pragma unroll
+                            for (int z = 0; z < 2; ++z) {
+                                terms_of<NK>(__uint_as_float(u[0][i + z]), __uint_as_float(u[1][i + z]), b0[z]);
+                                terms_of<NK>(__uint_as_float(u[2][i + z]), __uint_as_float(u[3][i + z]), b1[z]);
+                            }
                             products(4 * c + i, b0, b1);
                         }
                     }
