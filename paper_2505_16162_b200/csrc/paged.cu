@@ -108,7 +108,7 @@ template <int HD> knnssd_status launch_paged_rows(const attn::Args &a, int cache
 }
 
 template <int HD> void launch_rotary(const pages::RotaryArgs &a, int dtype, int cache_dtype, cudaStream_t s) {
-    const dim3 grid(a.n_rows), block(pages::ROT_NT);
+    const dim3 grid(a.n_rows), block(a.n_rows > pages::ROT_ROWS ? pages::ROT_FEW : pages::ROT_MANY);
     if (dtype == 1) launch_chained(pages::rotary_store_kernel<HD, bf16_t, bf16_t>, grid, block, 0, s, a);
     else if (cache_dtype == 1) launch_chained(pages::rotary_store_kernel<HD, float, bf16_t>, grid, block, 0, s, a);
     else launch_chained(pages::rotary_store_kernel<HD, float, float>, grid, block, 0, s, a);
