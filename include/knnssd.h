@@ -436,19 +436,23 @@ knnssd_status knnssd_page_tables(const int *lens_dev, const int *fresh_dev, int 
  * c x[i] - s x[i + hd/2] and c x[i + hd/2] + s x[i], in fp32.
  *   cos_sin_dev  DEVICE fp32 [n_positions][head_dim / 2][2]
  *   q_dev        DEVICE [n_rows][n_heads][head_dim], dtype: the rotated q; zeros for a row whose position is outside [0, n_positions)
+ *   k_rows_dev   DEVICE [n_rows][n_kv_heads][head_dim], dtype, or NULL: the rotated k by rows, as knnssd_packed_attention reads it; zeros likewise
  *   k_pages_dev, v_pages_dev  DEVICE, cache_dtype (rounded to nearest even): row r's go to row_slot[r]; nothing is stored for a row
  *                whose position or slot is out of range (-1: padding).  Two rows of one call may not have the same slot.
  */
 knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, long long row_stride, int n_heads,
                                   int n_kv_heads, int head_dim, const float *cos_sin_dev, int n_positions,
                                   const int *row_pos_dev, const int *row_slot_dev, int page_size, int n_pages, void *q_dev,
-                                  void *k_pages_dev, void *v_pages_dev, int cache_dtype, void *cuda_stream);
+                                  void *k_rows_dev, void *k_pages_dev, void *v_pages_dev, int cache_dtype, void *cuda_stream);
 
 /*
  * Attention of the new rows over the pages: row i of request b (row row_start[b] + i of q) looks at the positions 0 .. lens[b] + i, whose K
  * and V - its own among them - are in the pages.  out = sum_j softmax_j(scale q . k_j) v_j.
  *   q_dev    DEVICE [n_rows][n_heads][head_dim], rows q_stride elements apart;  out_dev DEVICE [n_rows][n_heads][head_dim], dtype
- *   max_fresh  the most rows a request has in this call, 0 if the host does not know: which kernels are launched goes by it, never the result
+ *   max_fresh  the most rows a request has in this call, 0 if the host does not know; a hint, the same kernels serve both (negative:
+ *              KNNSSD_ERR_INVALID_ARG)
+ *   scale      finite and not negative, else KNNSSD_ERR_INVALID_ARG; 0 gives equal weights
+ *   n_rows * n_heads below 2^31, else KNNSSD_ERR_CAPACITY
  * Positions whose page id is outside [0, n_pages) are not seen; a row that sees nothing gives zeros, and so do rows at and behind
  * row_start[n_requests].  What a row does not see never reaches it, not even NaN.  fp32 rows: 24-bit products, fp32 sums; bf16 rows: the softmax
  * weights are rounded to bf16 for the product with V.  Runs of positions that go to one warp follow from all lengths of the call: a row's
@@ -465,7 +469,7 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
  * row_start[b] + i.  Prompts may be empty.
  *   q_dev, k_dev, v_dev  DEVICE [n_rows][heads][head_dim] of one type, rows *_stride elements apart (views of one map's output serve)
  *   out_dev              DEVICE [n_rows][n_heads][head_dim], same type
- * Rounding, empty rows and rows behind the last prompt as in knnssd_paged_attention.
+ * Scale, limits, rounding, empty rows and rows behind the last prompt as in knnssd_paged_attention.
  */
 knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, const void *v_dev, int dtype, int n_rows,
                                       long long q_stride, long long k_stride, long long v_stride, int n_heads, int n_kv_heads,

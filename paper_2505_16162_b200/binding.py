@@ -90,7 +90,7 @@ def _load():
         "knnssd_spec_accept": (I, [P, P, P, I, I, P, F, PI, PI, P]),
         "knnssd_decode_sampled": (I, [P, I, I, F, F, P, I, P, PI, P, C.POINTER(Stats)]),
         "knnssd_page_tables": (I, [P, P, I, I, I, I, P, P, P, P, I, P, P, P, P, P, P]),
-        "knnssd_rotary_store": (I, [P, I, I, L, I, I, I, P, I, P, P, I, I, P, P, P, I, P]),
+        "knnssd_rotary_store": (I, [P, I, I, L, I, I, I, P, I, P, P, I, I, P, P, P, P, I, P]),
         "knnssd_paged_attention": (I, [P, I, I, L, I, I, I, P, P, I, I, I, P, I, P, P, I, I, F, P, P]),
         "knnssd_packed_attention": (I, [P, P, P, I, I, L, L, L, I, I, I, P, I, F, P, P]),
     }
@@ -343,9 +343,10 @@ def rotary_table(n_positions: int, head_dim: int, theta: float, device="cuda") -
 
 
 def knnssd_rotary_store(qkv: torch.Tensor, cos_sin: torch.Tensor, row_pos: torch.Tensor, row_slot: torch.Tensor, k_pages: torch.Tensor,
-                        v_pages: torch.Tensor, q: Optional[torch.Tensor] = None) -> torch.Tensor:
+                        v_pages: torch.Tensor, q: Optional[torch.Tensor] = None, k_rows: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotates the q and k heads of the rows of qkv [rows][(n_heads + 2 n_kv_heads) head_dim] by their positions, puts K and V into their
-    slots and returns q [rows][n_heads][head_dim] in qkv's type."""
+    slots and returns q [rows][n_heads][head_dim] in qkv's type; k_rows [rows][n_kv_heads][head_dim] of that type, if given, receives the
+    rotated K as knnssd_packed_attention reads it."""
     dev = _device(qkv)
     n_pages, kv, page, hd = _pages(k_pages, v_pages, dev)
     dtype, cache = _type(qkv, "qkv"), _type(k_pages, "k_pages")
@@ -359,9 +360,11 @@ def knnssd_rotary_store(qkv: torch.Tensor, cos_sin: torch.Tensor, row_pos: torch
         q = torch.empty((rows, heads, hd), dtype=qkv.dtype, device=qkv.device)
     elif q.shape != (rows, heads, hd) or q.dtype is not qkv.dtype or q.get_device() != dev or not q.is_contiguous():
         raise ValueError("q must be a contiguous tensor [rows][n_heads][head_dim] of qkv's type on its device")
+    if k_rows is not None and (k_rows.shape != (rows, kv, hd) or k_rows.dtype is not qkv.dtype or k_rows.get_device() != dev or not k_rows.is_contiguous()):
+        raise ValueError("k_rows must be a contiguous tensor [rows][n_kv_heads][head_dim] of qkv's type on its device")
     _call(_lib.knnssd_rotary_store, "knnssd_rotary_store", dev, qkv.data_ptr(), dtype, rows, qkv.stride(0) if rows > 1 else width, heads, kv, hd,
           cos_sin.data_ptr(), cos_sin.shape[0], _i32(row_pos, rows, dev, "row_pos"), _i32(row_slot, rows, dev, "row_slot"), page, n_pages, q.data_ptr(),
-          k_pages.data_ptr(), v_pages.data_ptr(), cache)
+          None if k_rows is None else k_rows.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), cache)
     return q
 
 
@@ -377,7 +380,7 @@ def knnssd_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
                            row_start: torch.Tensor, max_fresh: int = 0, scale: Optional[float] = None,
                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the new rows q [rows][n_heads][head_dim] over the requests' pages: row row_start[b] + i sees positions 0 .. lens[b] + i.
-    table [B][max_pages], lens [B], row_start [B + 1] int32.  max_fresh: the most rows of a request in this call, if known.  scale defaults to
+    table [B][max_pages], lens [B], row_start [B + 1] int32.  max_fresh: the most rows of a request in this call, if known (a hint).  scale defaults to
     head_dim ** -0.5."""
     dev = _device(q)
     n_pages, kv, page, hd = _pages(k_pages, v_pages, dev)

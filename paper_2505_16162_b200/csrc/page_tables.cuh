@@ -13,6 +13,9 @@ namespace pages {
 constexpr int NT = 1024;                  // threads of the planning block
 constexpr int MAX_REQUESTS = 8192;        // three prefixes of 32 KB each in shared memory
 constexpr int ROWS_NT = 256;
+// Rows up to which the planning block maps them itself, rather than a second launch over the whole chip: 120 / 500 / 1000 / 2000 / 4000 rows in
+// 7.2 / 7.6 / 8.0 / 9.5 / 12.2 us by itself, 8.7 / 9.5 / 10.0 / 10.6 / 11.5 with the launch; 30 000 rows 49 and 14.
+constexpr int ROWS_HERE = 3200;
 
 enum { SHORT_OF_PAGES = 1, TABLE_FULL = 2, TOO_MANY_ROWS = 4, BAD_STATE = 8 };
 
@@ -162,9 +165,9 @@ __global__ void __launch_bounds__(ROWS_NT) map_rows_kernel(const PlanArgs a) {
 // ---- rotary embedding of new rows, K and V into their pages ----------------------------------------------------------
 // A row of qkv is [n_heads + 2 n_kv_heads][hd]: q, k and v heads.  With (c, s) of the row's position and dimension i < hd / 2,
 //   x'[i] = c x[i] - s x[i + hd/2],  x'[i + hd/2] = c x[i + hd/2] + s x[i]
-// for q and k, in fp32; q goes to q_out, K and V, rounded to the cache's type (to nearest even), to the row's slot.  Every value is read
-// and written once: bound by memory.  A thread takes 16 bytes of either half of a head; the threads of a block keep their dimensions from
-// head to head, so the row's (c, s) are loaded once.
+// for q and k, in fp32; q goes to q_out (and K to k_rows, for attention over whole prompts), K and V, rounded to the cache's type (to nearest
+// even), to the row's slot.  Every value is read and written once: bound by memory.  A thread takes 16 bytes of either half of a head; the
+// threads of a block keep their dimensions from head to head, so the row's (c, s) are loaded once.
 struct RotaryArgs {
     const void *qkv;
     long long row_stride;                 // elements
@@ -172,7 +175,7 @@ struct RotaryArgs {
     const float2 *cos_sin;                // [n_positions][hd / 2]
     const int *row_pos, *row_slot;
     int page, n_slots;                    // n_slots = n_pages page
-    void *q_out, *k_pages, *v_pages;
+    void *q_out, *k_rows, *k_pages, *v_pages;      // k_rows: the rotated K heads by rows, or null
 };
 // A block does a row.  Few rows are done soonest by many threads each, many rows by few threads with more in flight each: 120 rows of 120 heads by 256 /
 // 128 / 64 threads 6.1 / 6.6 / 10.2 us, 8192 rows of 56 heads 48.2 / 42.0 / 39.7 (6.0 TB/s).
@@ -242,7 +245,7 @@ __global__ void __launch_bounds__(ROT_MANY) rotary_store_kernel(const RotaryArgs
         for (int u = 0; u < AHEAD; ++u) {
             const int h = h0 + u * STEP;
             const bool is_q = h < a.n_heads, is_v = h >= a.n_heads + a.n_kv_heads;
-            if (h >= heads || (!is_q && !stored)) continue;
+            if (h >= heads || (!is_q && !stored && (is_v || !a.k_rows))) continue;
             float v0[N], v1[N];
             unpack(lo[u], v0, (const XT *)nullptr);
             unpack(hi[u], v1, (const XT *)nullptr);
@@ -253,7 +256,14 @@ __global__ void __launch_bounds__(ROT_MANY) rotary_store_kernel(const RotaryArgs
                 XT *d = static_cast<XT *>(a.q_out) + ((size_t)row * a.n_heads + h) * HD + i0;
                 store_row(d, v0);
                 store_row(d + HD / 2, v1);
-            } else {
+                continue;
+            }
+            if (!is_v && a.k_rows) {
+                XT *d = static_cast<XT *>(a.k_rows) + ((size_t)row * a.n_kv_heads + h - a.n_heads) * HD + i0;
+                store_row(d, v0);
+                store_row(d + HD / 2, v1);
+            }
+            if (stored) {
                 const int kv = is_v ? h - a.n_heads - a.n_kv_heads : h - a.n_heads;
                 CT *d = static_cast<CT *>(is_v ? a.v_pages : a.k_pages) + ((page * a.n_kv_heads + kv) * a.page + off) * HD + i0;
                 store_row(d, v0);

@@ -146,26 +146,26 @@ knnssd_status knnssd_page_tables(const int *lens_dev, const int *fresh_dev, int 
     static bool configured[kMaxDevices] = {};
     if (!allow_smem(pages::plan_kernel, pages::plan_smem(pages::MAX_REQUESTS), configured)) return KNNSSD_ERR_CUDA;
     pages::PlanArgs a{lens_dev, fresh_dev, n_requests, page_size, max_pages, n_pages, owned_dev, table_dev, free_pages_dev, free_count_dev, max_rows,
-                      row_start_dev, row_request_dev, row_pos_dev, row_slot_dev, info_dev, max_rows <= 4096};
+                      row_start_dev, row_request_dev, row_pos_dev, row_slot_dev, info_dev, max_rows <= pages::ROWS_HERE};
     launch_chained(pages::plan_kernel, dim3(1), dim3(pages::NT), pages::plan_smem(n_requests), s, a);
     if (!a.rows_here) launch_chained(pages::map_rows_kernel, dim3((max_rows + pages::ROWS_NT - 1) / pages::ROWS_NT), dim3(pages::ROWS_NT), 0, s, a);
     return launched();
 }
 
 knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, long long row_stride, int n_heads, int n_kv_heads, int head_dim, const float *cos_sin_dev,
-                                  int n_positions, const int *row_pos_dev, const int *row_slot_dev, int page_size, int n_pages, void *q_dev, void *k_pages_dev,
-                                  void *v_pages_dev, int cache_dtype, void *cuda_stream) {
+                                  int n_positions, const int *row_pos_dev, const int *row_slot_dev, int page_size, int n_pages, void *q_dev,
+                                  void *k_rows_dev, void *k_pages_dev, void *v_pages_dev, int cache_dtype, void *cuda_stream) {
     if (n_rows < 0 || n_positions < 1) return KNNSSD_ERR_INVALID_ARG;
     if (knnssd_status st = check_heads(dtype, cache_dtype, n_heads, n_kv_heads, head_dim); st != KNNSSD_OK) return st;
     if (knnssd_status st = check_pages(page_size, 1, n_pages); st != KNNSSD_OK) return st;
     if (n_rows == 0) return KNNSSD_OK;
     if (!qkv_dev || !cos_sin_dev || !row_pos_dev || !row_slot_dev || !q_dev || !k_pages_dev || !v_pages_dev) return KNNSSD_ERR_INVALID_ARG;
     const long long width = ((long long)n_heads + 2ll * n_kv_heads) * head_dim;
-    if (row_stride < width || row_stride % (dtype ? 8 : 4) != 0 || !aligned16(qkv_dev) || !aligned16(cos_sin_dev) || !aligned16(q_dev) || !aligned16(k_pages_dev) ||
-        !aligned16(v_pages_dev))
+    if (row_stride < width || row_stride % (dtype ? 8 : 4) != 0 || !aligned16(qkv_dev) || !aligned16(cos_sin_dev) || !aligned16(q_dev) || !aligned16(k_rows_dev) ||
+        !aligned16(k_pages_dev) || !aligned16(v_pages_dev))
         return KNNSSD_ERR_SHAPE;
     pages::RotaryArgs a{qkv_dev, row_stride, n_rows, n_heads, n_kv_heads, n_positions, reinterpret_cast<const float2 *>(cos_sin_dev), row_pos_dev, row_slot_dev, page_size,
-                        n_pages * page_size, q_dev, k_pages_dev, v_pages_dev};
+                        n_pages * page_size, q_dev, k_rows_dev, k_pages_dev, v_pages_dev};
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     if (head_dim == 128) launch_rotary<128>(a, dtype, cache_dtype, s);
     else launch_rotary<64>(a, dtype, cache_dtype, s);

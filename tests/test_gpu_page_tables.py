@@ -241,3 +241,28 @@ def test_slots_beyond_32_bits_of_elements(kb):
     i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
     kb.knnssd_rotary_store(qkv, cs, i32([0, 0]), i32([n_pages * page - 1, n_pages * page - 2]), k, v)
     assert torch.equal(k[-1, :, -1], qkv[0].view(24, hd)[8:16]) and torch.equal(v[-1, :, -2], qkv[1].view(24, hd)[16:])
+
+
+@pytest.mark.parametrize("dtype,cache,H,KV,hd", [("fp32", "bf16", 4, 2, 64), ("bf16", "bf16", 40, 8, 128), ("fp32", "fp32", 3, 1, 128)])
+def test_rotated_k_by_rows(kb, dtype, cache, H, KV, hd):
+    rows, page = 37, 16
+    g = torch.Generator(device="cuda").manual_seed(H)
+    qkv = torch.randn(rows, (H + 2 * KV) * hd, generator=g, device="cuda").to(TYPES[dtype])
+    pos = torch.arange(100, 100 + rows, dtype=torch.int32, device="cuda")
+    slot = torch.arange(rows, dtype=torch.int32, device="cuda")
+    pos[3], pos[4], slot[5] = -1, 5000, -1                                   # no position twice, a position without a slot
+    cs = kb.rotary_table(5000, hd, 10000.0)
+    k, v = (torch.zeros(3, KV, page, hd, device="cuda", dtype=TYPES[cache]) for _ in range(2))
+    k0, v0 = k.clone(), v.clone()
+    q0 = kb.knnssd_rotary_store(qkv, cs, pos, slot, k0, v0)
+    got = torch.full((rows, KV, hd), float("nan"), device="cuda", dtype=TYPES[dtype])
+    q = kb.knnssd_rotary_store(qkv, cs, pos, slot, k, v, k_rows=got)
+    assert torch.equal(q, q0) and torch.equal(k, k0) and torch.equal(v, v0)  # nothing else changes by it
+    assert got[3:5].abs().max() == 0 and got[5].abs().max() > 0
+    by_slot = k.permute(0, 2, 1, 3).reshape(-1, KV, hd)                      # [slot][head][dim]
+    live = [r for r in range(rows) if r not in (3, 4, 5)]
+    assert torch.equal(got[live].to(TYPES[cache]), by_slot[live])
+    with pytest.raises(ValueError):
+        kb.knnssd_rotary_store(qkv, cs, pos, slot, k, v, k_rows=got[:, :, :32])
+    with pytest.raises(ValueError):
+        kb.knnssd_rotary_store(qkv, cs, pos, slot, k, v, k_rows=got.double())
