@@ -27,10 +27,9 @@ struct Args {
     float scale_log2;                     // scale log2 e: the softmax runs in powers of two
     int gs, subs, nvh;                    // query heads of an item; items that share a K/V head's rows (heads of a group / gs); KV subs
     int tb;                               // new rows of a block (of half a block, where blocks have two halves)
-    int pair_most;                        // positions up to which the halves of a block take two heads of a request with few rows
+    int pair;                             // the halves of a block take two heads of a request with few rows
     int extra;                            // positions that an item's beginning and end cost
-    int least_run;                        // positions a worker takes at least
-    int clear;                            // rows that no request has are this launch's to clear
+    int most, least_run;                  // workers at most (no more than the launch has); positions a worker takes at least
     // parts of items: what worker w knows of the item its run begins in, and its parts' (m, l) [w][SLOTS][rows] and o [w][SLOTS][rows][hd]
     struct Part *parts;
     float2 *ml;
@@ -42,7 +41,7 @@ struct Args {
 struct Part { long long start; int first, kv, from, to, row0, rows, vh, paired; };
 
 // A request's new rows n, what it held before, the block's rows tb and the items nvh per block.  HALVES: a block has two halves of a.tb rows each;
-// where a request has no more rows than one of them and few positions, the halves take two heads instead (paired).
+// where a request has no more rows than one of them, the halves may take two heads instead (paired).
 struct Request { int n, held, row0, tb, nvh; bool paired; long long cost; };
 
 template <bool HALVES> __device__ __forceinline__ Request request_here(const Args &a, int b) {
@@ -51,7 +50,7 @@ template <bool HALVES> __device__ __forceinline__ Request request_here(const Arg
     r.n = max(r1 - r0, 0);
     r.row0 = r0;
     r.held = a.lens ? (int)min((long long)max(a.lens[b], 0), (long long)a.max_pages << a.page_shift) : 0;
-    r.paired = HALVES && r.n <= a.tb && r.held + r.n <= a.pair_most;
+    r.paired = HALVES && a.pair && r.n <= a.tb;
     r.tb = HALVES && !r.paired ? 2 * a.tb : a.tb;
     r.nvh = r.paired ? (a.nvh + 1) / 2 : a.nvh;
     const long long whole = r.n / r.tb, left = r.n % r.tb, each = (long long)r.held + a.extra;
@@ -150,7 +149,7 @@ __device__ __forceinline__ long long run_start(long long total, int w, int W) { 
 template <int TP, bool HALVES> __device__ __forceinline__ int cut(const Item<HALVES> &it, long long x) {
     return (int)(x <= it.start ? 0 : min((x - it.start + TP - 1) & ~(long long)(TP - 1), (long long)it.kv));
 }
-__device__ __forceinline__ int workers_of(const Args &a, long long total, int most) { return (int)max(1ll, min((long long)most, total / a.least_run)); }
+__device__ __forceinline__ int workers_of(const Args &a, long long total) { return (int)max(1ll, min((long long)a.most, total / a.least_run)); }
 
 // What worker w leaves for the merge about the item that its run begins in.
 template <int TP, bool HALVES> __device__ __forceinline__ void note_part(const Args &a, const Item<HALVES> &it, int w, int W, long long total, long long x0, long long x1) {

@@ -49,11 +49,18 @@ template <int HD, typename KT, bool PAGED> knnssd_status launch_rows(attn::Args 
     a.subs = (G + a.gs - 1) / a.gs;
     a.nvh = a.KV * a.subs;
     a.tb = most / a.gs;
-    const int ctas = sm_count(), warps = ctas * Rg::WARPS;
+    // An item's beginning and end in positions, and what a warp takes at least: extra 0 / 64 / 256: 9 prompts of 3001 tokens 50 / 42 / 55 us, 8 requests
+    // of 5 new rows 56 / 58 / 66; least_run 16 / 32 / 64 / 256: 2 requests of 1851 positions 33 / 24 / 22 / -, one of 96 15 / 15 / 15 / 29.
+    a.extra = 64;
+    a.least_run = 64;
+    // Parts an item may be in, as the merge takes them 32 at a time: at most 32 / 64 / 128 / any number (296): one request of 31 009 positions 85 / 51 / 40 /
+    // 56 us, two of 74 011 205 / 119 / 87 / 105.
+    const int ctas = sm_count();
+    a.most = (int)std::min((long long)ctas * Rg::WARPS, 128ll * a.nvh * std::max(a.B, a.R / a.tb));
     Scratch mem(s);
-    if (!get_parts(mem, a, warps, most, HD)) return KNNSSD_ERR_CUDA;
+    if (!get_parts(mem, a, a.most, most, HD)) return KNNSSD_ERR_CUDA;
     launch_chained(kernel, dim3(ctas), dim3(Rg::WARPS * 32), Rg::SMEM, s, a);
-    launch_chained(attn::merge_kernel<HD, float, false, 16>, dim3(warps - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
+    launch_chained(attn::merge_kernel<HD, float, false, 16>, dim3(a.most - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
     return launched();
 }
 
@@ -79,7 +86,17 @@ template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, cudaStream
     a.subs = (G + a.gs - 1) / a.gs;
     a.nvh = a.KV * a.subs;
     a.tb = most / a.gs;
-    a.extra = 384; a.least_run = 512; a.pair_most = 1024;
+    const int ctas = sm_count();
+    // An item's beginning and end cost a CTA some 5 to 8 thousand clocks, as much as these positions: with 0 / 384 / 1024, 24 short prompts take
+    // 89 / 35 / 34 us and 12000 tokens in 4 prompts 943 / 729 / 776.
+    a.extra = 384;
+    // What a CTA takes at least: with 64 / 512 / 2048, 6 requests of 13 thousand positions take 33 / 32 / 42 us, 24 short prompts 35 / 35 / 40.
+    a.least_run = 512;
+    // Two heads a block where there are items enough for all CTAs either way: half as many beginnings and ends, half as many pieces.  1440 items
+    // of one row 44 -> 33 us, 768 of about 100 rows 43 -> 35, 512 of one row and 200 positions 46 -> 43; but 16 of 35 thousand positions 35 -> 45,
+    // 128 of 50 positions 22 -> 25.  One answer for the call: a head's positions cost a pair twice the reading, and a mix of both is uneven.
+    a.most = ctas;
+    a.pair = (long long)a.B * a.nvh >= 2ll * ctas;
     CUtensorMap qm{}, km{}, vm{};
     const cuuint64_t qs[3] = {HD, (cuuint64_t)a.H, (cuuint64_t)a.R}, qst[2] = {HD * 2, (cuuint64_t)a.q_stride * 2};
     const cuuint32_t qb[3] = {64, (cuuint32_t)a.gs, (cuuint32_t)a.tb};
@@ -95,7 +112,6 @@ template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, cudaStream
         made = made && bf16_map(&km, a.k, 3, ks, kst, kb) && bf16_map(&vm, a.v, 3, ks, vst, kb);
     }
     if (!made) return KNNSSD_ERR_CUDA;
-    const int ctas = sm_count();
     Scratch mem(s);
     if (!get_parts(mem, a, ctas, tcattn::ROWS, HD)) return KNNSSD_ERR_CUDA;
     launch_chained(kernel, dim3(ctas), dim3(tcattn::threads_of(MODE == tcattn::COPIED)), L::SMEM, s, a, qm, km, vm);
@@ -190,7 +206,6 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
     while ((1 << a.page_shift) < page_size) ++a.page_shift;
     a.lens = lens_dev; a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
     a.scale_log2 = log2_scale(scale);
-    a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if (dtype == 1) {
@@ -221,7 +236,6 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
     a.k = k_dev; a.v = v_dev; a.k_stride = k_stride; a.v_stride = v_stride;
     a.row_start = row_start_dev; a.B = n_requests; a.R = n_rows; a.H = n_heads; a.KV = n_kv_heads;
     a.scale_log2 = log2_scale(scale);
-    a.extra = 64; a.least_run = 64; a.clear = 1;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if (dtype == 1) {

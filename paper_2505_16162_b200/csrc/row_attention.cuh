@@ -71,14 +71,14 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     sum_costs<false>(a, costs);
-    if (a.clear) clear_tail<float>(a, HD, blockIdx.x * NT + threadIdx.x, gridDim.x * NT);
+    clear_tail<float>(a, HD, blockIdx.x * NT + threadIdx.x, gridDim.x * NT);
     const long long total = costs.pfx[NT];
-    const int W = workers_of(a, total, gridDim.x * Rg::WARPS);
+    const int W = workers_of(a, total);
     // neighbouring runs go to different SMs: a short launch spreads over the chip
     const int w = warp * gridDim.x + blockIdx.x;
     const long long x0 = w < W ? run_start(total, w, W) : 0, x1 = w < W ? run_start(total, w + 1, W) : 0;
     if (x0 >= x1) {
-        if (lane == 0) { a.parts[w].first = 0; a.parts[w].start = -1; }
+        if (lane == 0 && w < a.most) { a.parts[w].first = 0; a.parts[w].start = -1; }
         return;
     }
     Item<false> in = item_at<false>(a, costs, x0);                   // the item whose positions are being fetched

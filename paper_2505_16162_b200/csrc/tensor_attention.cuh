@@ -325,9 +325,9 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
     sum_costs<true>(a, costs);                                       // has the block's barriers
     fence_after();
     const uint32_t tmem = tmem_base;
-    if (a.clear) clear_tail<bf16_t>(a, HD, blockIdx.x * blockDim.x + tid, gridDim.x * blockDim.x);
+    clear_tail<bf16_t>(a, HD, blockIdx.x * blockDim.x + tid, gridDim.x * blockDim.x);
     const long long total = costs.pfx[NCOST];
-    const int w = blockIdx.x, W = total > 0 ? workers_of(a, total, gridDim.x) : 0;
+    const int w = blockIdx.x, W = total > 0 ? workers_of(a, total) : 0;
     const long long x0 = w < W ? run_start(total, w, W) : 0, x1 = w < W ? run_start(total, w + 1, W) : 0;
     if (x0 >= x1) {
         if (tid == 0) { a.parts[w].first = 0; a.parts[w].start = -1; }
