@@ -449,8 +449,8 @@ knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, lo
  * Attention of the new rows over the pages: row i of request b (row row_start[b] + i of q) looks at the positions 0 .. lens[b] + i, whose K
  * and V - its own among them - are in the pages.  out = sum_j softmax_j(scale q . k_j) v_j.
  *   q_dev    DEVICE [n_rows][n_heads][head_dim], rows q_stride elements apart;  out_dev DEVICE [n_rows][n_heads][head_dim], dtype
- *   max_fresh  the most rows a request has in this call, 0 if the host does not know; a hint, the same kernels serve both (negative:
- *              KNNSSD_ERR_INVALID_ARG)
+ *   max_fresh  the most rows a request has in this call, 0 if the host does not know: the size of a launch goes by it, never the result
+ *              (negative: KNNSSD_ERR_INVALID_ARG)
  *   scale      finite and not negative, else KNNSSD_ERR_INVALID_ARG; 0 gives equal weights
  *   n_rows * n_heads below 2^31, else KNNSSD_ERR_CAPACITY
  * Positions whose page id is outside [0, n_pages) are not seen; a row that sees nothing gives zeros, and so do rows at and behind

@@ -183,92 +183,98 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-// Items in parts.  Block (w, j) does eight rows, j 8 .., of the item that worker w's run is the first to begin within: the part of worker w - 1
+// Items in parts.  Block (w, j) does eight rows at a time of the item that worker w's run is the first to begin within: the part of worker w - 1
 // and those behind it until the item's end, in their order.  Of few rows each has several of the block's eight warps, which share its parts out;
-// a warp's lanes share the parts' (m, l) out, then hd / 32 dimensions each.
+// a warp's lanes share the parts' (m, l) out, then hd / 32 dimensions each.  The grid has as many j as the host believes there to be
+// rows, of either half; if there are more, a block goes on to them.  With as many as 256 rows need, whatever there is: 4 requests of 16 rows and 50
+// positions 23 us for 18, 33 of 2 rows 20 for 16, 2 of 35 361 positions 37 for 30 (12000 packed tokens 723 for 726: five blocks an SM either way).
 template <int HD, typename QT, bool HALVES, int ROWS>
-__global__ void __launch_bounds__(256) merge_kernel(const Args a) {
-    constexpr int D = HD / 32;
+__global__ void __launch_bounds__(256, 5) merge_kernel(const Args a) {
+    constexpr int D = HD / 32, HALF = HALVES ? ROWS / 2 : ROWS;
     __shared__ float2 ml_of[8];
     __shared__ float o_of[8][HD];
     chain_wait();
     const int w = blockIdx.x + 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const Part p = a.parts[w];
     if (!p.first) return;
-    const int rows = HALVES ? ROWS : min(ROWS, p.rows * a.gs), here = min(8, rows - (int)blockIdx.y * 8);
-    if (here <= 0) return;
-    const int share = here > 4 ? 1 : here > 2 ? 2 : here > 1 ? 4 : 8;            // warps a row
-    const int r = blockIdx.y * 8 + warp / share, mine = warp % share;
-    int token = -1, head = 0;
-    if (warp / share < here) place_of<HALVES, ROWS>(a, p.rows, p.vh, p.paired, r, token, head);
-    // part i: of run w - 1 + i, as long as the runs begin in this item
-    auto slot = [&](int i) { return ((size_t)(w - 1 + i) * SLOTS + (i == 0 ? 1 : 0)) * ROWS + r; };
-    const int most = gridDim.x + 2 - w;
-    float o[D], m = -INFINITY, l = 0.f;
+    const int step = HALVES ? gridDim.y / 2 : gridDim.y, half = blockIdx.y / step;
+    // the half's rows that can be live; place_of leaves out those of them that are not
+    const int rows = min(HALF, (HALVES && !p.paired ? min(a.tb, p.rows - half * a.tb) : p.rows) * a.gs);
+    for (int r0 = blockIdx.y % step * 8; r0 < rows; r0 += step * 8) {
+        const int here = min(8, rows - r0);
+        const int share = here > 4 ? 1 : here > 2 ? 2 : here > 1 ? 4 : 8;            // warps a row
+        const int r = half * HALF + r0 + warp / share, mine = warp % share;
+        int token = -1, head = 0;
+        if (warp / share < here) place_of<HALVES, ROWS>(a, p.rows, p.vh, p.paired, r, token, head);
+        // part i: of run w - 1 + i, as long as the runs begin in this item
+        auto slot = [&](int i) { return ((size_t)(w - 1 + i) * SLOTS + (i == 0 ? 1 : 0)) * ROWS + r; };
+        const int most = gridDim.x + 2 - w;
+        float o[D], m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int i = 0; i < D; ++i) o[i] = 0.f;
-    for (int i0 = mine * 32; token >= 0; i0 += 32 * share) {
-        const int i = i0 + lane;
-        bool its = i < most, there = its;                            // there: not cut away
-        if (its && i > 0) {
-            const Part *q = a.parts + w - 1 + i;
-            its = q->start == p.start;
-            there = its && q->from < q->to;
-        }
-        const unsigned all = __ballot_sync(0xffffffffu, its);
-        const int n = all == 0xffffffffu ? 32 : __ffs(~all) - 1;      // lanes up to the first that is not of the item
-        there = there && lane < n;
-        const float2 v = there ? a.ml[slot(i)] : make_float2(-INFINITY, 0.f);
-        const float mn = fmaxf(m, warp_max(v.x)), base = mn == -INFINITY ? 0.f : mn;
-        const float f = exp2_approx(v.x - base), old = exp2_approx(m - base);
-        l = l * old + warp_sum(v.y * f);
-#pragma unroll
-        for (int j = 0; j < D; ++j) o[j] *= old;
-        m = mn;
-        const unsigned some = __ballot_sync(0xffffffffu, there);
-#pragma unroll 8
-        for (int u = 0; u < n; ++u) {
-            const float fu = __shfl_sync(0xffffffffu, f, u);
-            float d[D];
-#pragma unroll
-            for (int j = 0; j < D; ++j) d[j] = 0.f;
-            if (some >> u & 1) {
-                const float *src = a.o + slot(i0 + u) * HD + lane * D;
-                if constexpr (D == 4) {
-                    const float4 v4 = *reinterpret_cast<const float4 *>(src);
-                    d[0] = v4.x; d[1] = v4.y; d[2] = v4.z; d[3] = v4.w;
-                } else {
-                    const float2 v2 = *reinterpret_cast<const float2 *>(src);
-                    d[0] = v2.x; d[1] = v2.y;
-                }
+        for (int i = 0; i < D; ++i) o[i] = 0.f;
+        for (int i0 = mine * 32; token >= 0; i0 += 32 * share) {
+            const int i = i0 + lane;
+            bool its = i < most, there = its;                            // there: not cut away
+            if (its && i > 0) {
+                const Part *q = a.parts + w - 1 + i;
+                its = q->start == p.start;
+                there = its && q->from < q->to;
             }
+            const unsigned all = __ballot_sync(0xffffffffu, its);
+            const int n = all == 0xffffffffu ? 32 : __ffs(~all) - 1;      // lanes up to the first that is not of the item
+            there = there && lane < n;
+            const float2 v = there ? a.ml[slot(i)] : make_float2(-INFINITY, 0.f);
+            const float mn = fmaxf(m, warp_max(v.x)), base = mn == -INFINITY ? 0.f : mn;
+            const float f = exp2_approx(v.x - base), old = exp2_approx(m - base);
+            l = l * old + warp_sum(v.y * f);
 #pragma unroll
-            for (int j = 0; j < D; ++j) o[j] = fmaf(fu, d[j], o[j]);
-        }
-        if (n < 32) break;
-    }
-    if (share > 1) {                                                 // the row's warps, in their order
-        if (lane == 0) ml_of[warp] = make_float2(m, l);
-#pragma unroll
-        for (int j = 0; j < D; ++j) o_of[warp][lane * D + j] = o[j];
-        __syncthreads();
-        if (mine > 0) return;
-        for (int u = 1; u < share; ++u) {
-            const float2 v = ml_of[warp + u];
-            const float mn = fmaxf(m, v.x), base = mn == -INFINITY ? 0.f : mn, f = exp2_approx(v.x - base), old = exp2_approx(m - base);
+            for (int j = 0; j < D; ++j) o[j] *= old;
             m = mn;
-            l = l * old + v.y * f;
+            const unsigned some = __ballot_sync(0xffffffffu, there);
+#pragma unroll 8
+            for (int u = 0; u < n; ++u) {
+                const float fu = __shfl_sync(0xffffffffu, f, u);
+                float d[D];
 #pragma unroll
-            for (int j = 0; j < D; ++j) o[j] = o[j] * old + f * o_of[warp + u][lane * D + j];
+                for (int j = 0; j < D; ++j) d[j] = 0.f;
+                if (some >> u & 1) {
+                    const float *src = a.o + slot(i0 + u) * HD + lane * D;
+                    if constexpr (D == 4) {
+                        const float4 v4 = *reinterpret_cast<const float4 *>(src);
+                        d[0] = v4.x; d[1] = v4.y; d[2] = v4.z; d[3] = v4.w;
+                    } else {
+                        const float2 v2 = *reinterpret_cast<const float2 *>(src);
+                        d[0] = v2.x; d[1] = v2.y;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < D; ++j) o[j] = fmaf(fu, d[j], o[j]);
+            }
+            if (n < 32) break;
         }
-    }
-    if (token < 0) return;
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    QT *d = static_cast<QT *>(a.out) + ((size_t)(p.row0 + token) * a.H + head) * HD + lane * D;
+        if (share > 1) {                                                 // the row's warps, in their order
+            if (lane == 0) ml_of[warp] = make_float2(m, l);
 #pragma unroll
-    for (int j = 0; j < D; j += 2) {
-        if constexpr (sizeof(QT) == 2) *reinterpret_cast<uint32_t *>(d + j) = cvt_bf16x2(o[j] * inv, o[j + 1] * inv);
-        else *reinterpret_cast<float2 *>(d + j) = make_float2(o[j] * inv, o[j + 1] * inv);
+            for (int j = 0; j < D; ++j) o_of[warp][lane * D + j] = o[j];
+            __syncthreads();
+            for (int u = 1; u < share && mine == 0; ++u) {
+                const float2 v = ml_of[warp + u];
+                const float mn = fmaxf(m, v.x), base = mn == -INFINITY ? 0.f : mn, f = exp2_approx(v.x - base), old = exp2_approx(m - base);
+                m = mn;
+                l = l * old + v.y * f;
+#pragma unroll
+                for (int j = 0; j < D; ++j) o[j] = o[j] * old + f * o_of[warp + u][lane * D + j];
+            }
+            __syncthreads();                                             // before the next rows
+        }
+        if (token < 0 || mine > 0) continue;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        QT *d = static_cast<QT *>(a.out) + ((size_t)(p.row0 + token) * a.H + head) * HD + lane * D;
+#pragma unroll
+        for (int j = 0; j < D; j += 2) {
+            if constexpr (sizeof(QT) == 2) *reinterpret_cast<uint32_t *>(d + j) = cvt_bf16x2(o[j] * inv, o[j + 1] * inv);
+            else *reinterpret_cast<float2 *>(d + j) = make_float2(o[j] * inv, o[j + 1] * inv);
+        }
     }
 }
 

@@ -75,7 +75,8 @@ int *attention_err_ptr() {
     return addr[dev];
 }
 
-template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, cudaStream_t s) {
+// most_rows: the rows that a request is believed to have at most.
+template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, int most_rows, cudaStream_t s) {
     using L = tcattn::Lay<HD>;
     static bool configured[kMaxDevices] = {};
     const auto kernel = tcattn::tensor_kernel<HD, MODE>;
@@ -115,7 +116,7 @@ template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, cudaStream
     Scratch mem(s);
     if (!get_parts(mem, a, ctas, tcattn::ROWS, HD)) return KNNSSD_ERR_CUDA;
     launch_chained(kernel, dim3(ctas), dim3(tcattn::threads_of(MODE == tcattn::COPIED)), L::SMEM, s, a, qm, km, vm);
-    launch_chained(attn::merge_kernel<HD, bf16_t, true, tcattn::ROWS>, dim3(ctas - 1, tcattn::ROWS / 8), dim3(256), 0, s, a);
+    launch_chained(attn::merge_kernel<HD, bf16_t, true, tcattn::ROWS>, dim3(ctas - 1, 2 * ((std::min(a.tb, most_rows) * a.gs + 7) / 8)), dim3(256), 0, s, a);
     return launched();
 }
 
@@ -209,10 +210,11 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if (dtype == 1) {
+            const int most_rows = max_fresh > 0 ? std::min(max_fresh, a.R) : a.R;
             // a coordinate of the TMA has 31 bits
             if (page_size >= 64 && (long long)n_pages * page_size * n_kv_heads <= INT_MAX)
-                return head_dim == 128 ? launch_tensor<128, tcattn::TILED>(a, s) : launch_tensor<64, tcattn::TILED>(a, s);
-            return head_dim == 128 ? launch_tensor<128, tcattn::COPIED>(a, s) : launch_tensor<64, tcattn::COPIED>(a, s);
+                return head_dim == 128 ? launch_tensor<128, tcattn::TILED>(a, most_rows, s) : launch_tensor<64, tcattn::TILED>(a, most_rows, s);
+            return head_dim == 128 ? launch_tensor<128, tcattn::COPIED>(a, most_rows, s) : launch_tensor<64, tcattn::COPIED>(a, most_rows, s);
         }
         return head_dim == 128 ? launch_paged_rows<128>(a, cache_dtype, s) : launch_paged_rows<64>(a, cache_dtype, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }
@@ -239,7 +241,7 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if (dtype == 1) {
-            return head_dim == 128 ? launch_tensor<128, tcattn::PACKED>(a, s) : launch_tensor<64, tcattn::PACKED>(a, s);
+            return head_dim == 128 ? launch_tensor<128, tcattn::PACKED>(a, a.R, s) : launch_tensor<64, tcattn::PACKED>(a, a.R, s);
         }
         return head_dim == 128 ? launch_rows<128, float, false>(a, s) : launch_rows<64, float, false>(a, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }

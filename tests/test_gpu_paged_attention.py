@@ -377,3 +377,13 @@ def test_refusals(kb):
     assert status(kb.knnssd_packed_attention, ragged, k, v, start) == 2       # rows that are no multiple of 16 bytes apart
     none = kb.knnssd_packed_attention(q[:0], k[:0], v[:0], start)
     assert none.shape == (0, 4, 64)                                  # no rows: nothing to do
+
+
+@pytest.mark.parametrize("dtype,cache", KINDS)
+@pytest.mark.parametrize("KV,lens,fresh", [(2, [30011, 5000], [60, 3]), (8, [700] * 39 + [9000], [2] * 38 + [200, 1])])
+def test_a_hint_that_is_too_low_changes_nothing(kb, dtype, cache, KV, lens, fresh):
+    p = Paged(23, lens, fresh, KV, 128, 64, cache)
+    q = p.q(4 * KV, 128, dtype)
+    got = p.run(kb, q, max_fresh=1)
+    _check(got, *p.want(q))
+    assert torch.equal(got, p.run(kb, q)) and torch.equal(got, p.run(kb, q, max_fresh=300))
