@@ -186,14 +186,15 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+// The largest of three; NaN where one is.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 // 2^x of two values on the multiply-add units: x = n + f with n the nearest whole number (added to 1.5 2^23 it is the sum's low bits), 2^f by a
 // cubic (minimax of the relative error on [-1/2, 1/2] by Lawson's weighted least squares: 7.5e-5, an eighth of what rounding to bf16
-// does at most), and n added to the exponent.  Below 2^-126 it gives 2^-126: next to nothing, but not nothing.
+// does at most), and n added to the exponent.  Below 2^-126 it gives 2^-126: next to nothing, but not nothing; so does NaN.
 __device__ __forceinline__ void exp2_cubic(uint64_t x, float &a, float &b) {
     float x0, x1;
     split(x, x0, x1);
@@ -623,7 +624,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                     float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                     for (int i = 0; i < SUB; i += 2) tops[(i >> 1) & 3] = max3(tops[(i >> 1) & 3], __uint_as_float(x[i >> 5][i & 31]), __uint_as_float(x[i >> 5][(i & 31) + 1]));
-                    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                    const float top = max3(max3(tops[0], tops[1], tops[2]), tops[3], tops[3]);
                     const float grown = top == -INFINITY ? -INFINITY : top * a.scale_log2;
                     const bool over = grown > m + GROWTH;            // the first positions a row sees: m is -inf
                     if (__any_sync(0xffffffffu, over)) {
@@ -645,6 +646,8 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                             }
                         }
                     }
+                    // A score that is NaN or +inf makes the row NaN (inf - inf).  Its weight need not show it, the cubic has no NaN: l does, from here on.
+                    if (!(top < INFINITY)) l = __int_as_float(0x7fffffff);
                     const float base = m == -INFINITY ? 0.f : m;
                     uint64_t sums[2] = {0, 0};
                     const uint64_t scale2 = pair_of(a.scale_log2, a.scale_log2), base2 = pair_of(-base, -base);
@@ -681,7 +684,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                     fence_after();
                 }
                 if (live && (steps || (job.from < job.to && !whole))) {
-                    const bool none = m == -INFINITY;                // the row has seen nothing
+                    const bool none = m == -INFINITY && l == l;      // the row has seen nothing
                     if (none) l = 0.f;
                     const float f = none ? 0.f : whole ? __fdividef(1.0f, l) : 1.f;
                     const size_t slot = ((size_t)w * SLOTS + (job.from > 0 ? 0 : 1)) * ROWS;

@@ -1,0 +1,80 @@
+"""Attention of new rows where scores or values are not finite, or large, against the definition: a row's result follows from what it sees.
+
+A score that is NaN or +inf makes its row NaN; one of -inf has the weight 0; what a row does not see has no part in it, whatever it holds.
+Tolerances of finite results are those of test_gpu_paged_attention.py.
+"""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_paged_attention import Paged, _attend64, _check, _packed
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def kb():
+    if not torch.cuda.is_available():
+        pytest.fail("the gpu tests need a CUDA device")
+    from paper_2505_16162_b200 import build
+    build.build()
+    from paper_2505_16162_b200 import binding
+    return binding
+
+
+def _by_scores(q, k, v, seen, scale):
+    """_attend64 where scores may be anything: (result, tolerance)."""
+    n, H, hd = q.shape
+    outs = []
+    for h in range(H):
+        kh, vh = (x[:, h * k.shape[1] // H][:, None] for x in (k, v))
+        s = torch.where(seen, torch.stack([(q[i, h].double()[None] * kh[:, 0].double()).sum(1) for i in range(n)]) * scale, -torch.inf)
+        o, t = _attend64(q[:, h:h + 1], kh, vh, seen & s.isfinite(), scale)
+        o[(s.isnan() | (s == torch.inf)).any(1)] = torch.nan
+        outs.append((o, t))
+    return torch.cat([o for o, _ in outs], 1), torch.cat([t for _, t in outs], 1)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("lens,first,page", [(20, 0, 16), (20, 8, 64), (300, 128, 64), (300, 256, 16)])
+def test_keys_that_are_not_finite_bf16(kb, value, lens, first, page):
+    p = Paged(41, [lens] * 16, [6] * 16, 2, 64, page, "bf16")
+    for b in range(16):                                              # one position of each request, all places modulo 16
+        at = first + b
+        p.k[int(p.table[b, at // page]), 1, at % page, 7] = value
+        p.dense[b][0][at, 1, 7] = value
+    q = p.q(4, 64, "bf16")
+    got = p.run(kb, q)
+    for b in range(16):
+        r = slice(6 * b, 6 * b + 6)
+        want, tol = _by_scores(q[r], *p.dense[b], p.seen(b), 64 ** -0.5)
+        assert want.isnan().any() and not want.isnan().all()
+        _check(got[r], want, tol, f"position {first + b}")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_queries_that_are_nan_in_first_rows(kb, dtype):
+    lens = [1, 2, 2, 3, 40, 9]
+    q, k, v, start = _packed(43, lens, 4, 2, 64, dtype)
+    for b, i in ((0, 0), (1, 0), (2, 1), (3, 1), (4, 0), (5, 8)):
+        q[int(start[b]) + i, 1 + b % 3, 11] = torch.nan
+    got = kb.knnssd_packed_attention(q, k, v, start)
+    for b, n in enumerate(lens):
+        r = slice(int(start[b]), int(start[b]) + n)
+        _check(got[r], *_by_scores(q[r], k[r], v[r], torch.ones(n, n, dtype=torch.bool, device="cuda").tril(), 64 ** -0.5), f"prompt {b}")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_rows_of_nan_alone_in_parts(kb, dtype):
+    """A context that several workers share: the joined row is NaN whichever part has the score."""
+    p = Paged(47, [40000], [2], 1, 128, 64, dtype)
+    for at in (0, 1, 17, 20000, 39999):
+        page, off = int(p.table[0, at // 64]), at % 64
+        old = p.k[page, 0, off, 0].clone()
+        p.k[page, 0, off, 0] = torch.nan
+        q = p.q(2, 128, dtype)
+        assert p.run(kb, q).isnan().all(), f"position {at}"
+        p.k[page, 0, off, 0] = old
+    q[0, 1, 5] = torch.nan
+    got = p.run(kb, q)
+    assert got[0, 1].isnan().all() and got[0, 0].isfinite().all() and got[1].isfinite().all()
