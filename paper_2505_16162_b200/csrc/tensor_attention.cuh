@@ -181,6 +181,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     uint64_t d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -192,22 +197,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// 2^x of two values on the multiply-add units: x = n + f with n the nearest whole number (added to 1.5 2^23 it is the sum's low bits), 2^f by a
-// cubic (minimax of the relative error on [-1/2, 1/2] by Lawson's weighted least squares: 7.5e-5, an eighth of what rounding to bf16
-// does at most), and n added to the exponent.  Below 2^-126 it gives 2^-126: next to nothing, but not nothing; so does NaN.
+// 2^x of two values on the multiply-add units: x = n + f with n the nearest whole number (added to 1.5 2^23 + 127 it is the sum's low bits, biased as
+// an exponent is), 2^f by a cubic (minimax of the relative error on [-1/2, 1/2] by Lawson's weighted least squares: 7.5e-5, a fiftieth of what
+// rounding to bf16 does at most), times 2^n.  n = -127 stands for 0, so that what a row does not see has no weight at all; NaN gives 0 as well.
 __device__ __forceinline__ void exp2_cubic(uint64_t x, float &a, float &b) {
     float x0, x1;
     split(x, x0, x1);
-    x = pair_of(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-    const uint64_t n = add2(x, pair_of(12582912.f, 12582912.f)), f = fma2(add2(n, pair_of(-12582912.f, -12582912.f)), pair_of(-1.f, -1.f), x);
+    x = pair_of(fmaxf(x0, -127.f), fmaxf(x1, -127.f));
+    const uint64_t n = add2(x, pair_of(12583039.f, 12583039.f)), f = fma2(add2(n, pair_of(-12583039.f, -12583039.f)), pair_of(-1.f, -1.f), x);
     uint64_t y = fma2(f, pair_of(0.0551716685295105f, 0.0551716685295105f), pair_of(0.2426111251115799f, 0.2426111251115799f));
     y = fma2(f, y, pair_of(0.6932609677314758f, 0.6932609677314758f));
     y = fma2(f, y, pair_of(0.9999280571937561f, 0.9999280571937561f));
-    float y0, y1, n0, n1;
-    split(y, y0, y1);
+    float n0, n1;
     split(n, n0, n1);
-    a = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(n0) << 23));
-    b = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(n1) << 23));
+    split(mul2(y, pair_of(__float_as_uint(n0) << 23, __float_as_uint(n1) << 23)), a, b);
 }
 
 // Lane 4 i + j has row j of a 4 x 4 square of 16-byte pieces; afterwards it has column j.

@@ -78,3 +78,36 @@ def test_rows_of_nan_alone_in_parts(kb, dtype):
     q[0, 1, 5] = torch.nan
     got = p.run(kb, q)
     assert got[0, 1].isnan().all() and got[0, 0].isfinite().all() and got[1].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,cache", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("page", [16, 64])
+def test_large_values_that_are_not_seen(kb, dtype, cache, page):
+    """The last new row's V is near the type's largest, all places modulo 16: the rows before it are as if it were not there."""
+    p = Paged(53, [60 + b for b in range(16)], [4] * 16, 2, 64, page, cache)
+    for b in range(16):
+        at = p.lens[b] + 3
+        p.v[int(p.table[b, at // page]), :, at % page] = 3e38
+        p.dense[b][1][at] = 3e38
+    q = p.q(4, 64, dtype)
+    got = p.run(kb, q)
+    for b in range(16):
+        r = slice(4 * b, 4 * b + 3)
+        seen = p.seen(b)[:3, :-1]
+        _check(got[r], *_attend64(q[r], p.dense[b][0][:-1], p.dense[b][1][:-1], seen, 64 ** -0.5), f"request {b}")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_scores_far_below_the_largest_weigh_nothing(kb, dtype):
+    """Scores 400 powers of two below the row's largest, at all places modulo 8 but one: their large V have no part in the result."""
+    lens = [9] * 8
+    q, k, v, start = _packed(59, lens, 2, 2, 64, dtype)
+    q[:], k[:] = 0.0, 0.0
+    q[:, :, 0], k[:, :, 0] = 8.0, -277.0                             # scale 1/8: scores -277, or 0 at one position: 2^-399.6
+    v[:] = 3e38
+    for b in range(8):
+        k[9 * b + b, :, 0] = 0.0
+        v[9 * b + b] = 1.5
+    got = kb.knnssd_packed_attention(q, k, v, start)
+    for b in range(8):
+        assert (got[9 * b + b:9 * b + 9] == 1.5).all(), f"position {b}"
