@@ -183,6 +183,104 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
+// ---- rows by the definition ------------------------------------------------------------------------------------------
+// Where a position of a request's K/V head lies, in elements; false: it has no page.
+template <int HD, bool PAGED> __device__ __forceinline__ bool key_at(const Args &a, int b, int seq_row0, int kvh, int pos, size_t &k, size_t &v) {
+    if (!PAGED) {
+        k = (size_t)(seq_row0 + pos) * a.k_stride + (size_t)kvh * HD;
+        v = (size_t)(seq_row0 + pos) * a.v_stride + (size_t)kvh * HD;
+        return true;
+    }
+    const int idx = pos >> a.page_shift, id = idx < a.max_pages ? a.table[(size_t)b * a.max_pages + idx] : -1;
+    if (id < 0 || id >= a.n_pages) return false;
+    k = v = ((((size_t)id * a.KV + kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1))) * HD;
+    return true;
+}
+// N words, by as many bytes at a time as they are a multiple of.
+template <int N> __device__ __forceinline__ void read_words(const void *p, uint32_t (&w)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 u = __ldg(static_cast<const uint4 *>(p) + i / 4);
+            w[i] = u.x; w[i + 1] = u.y; w[i + 2] = u.z; w[i + 3] = u.w;
+        }
+    } else if constexpr (N == 2) {
+        const uint2 u = __ldg(static_cast<const uint2 *>(p));
+        w[0] = u.x; w[1] = u.y;
+    } else w[0] = __ldg(static_cast<const uint32_t *>(p));
+}
+template <int N> __device__ __forceinline__ void read_values(const float *p, float (&v)[N]) {
+    uint32_t w[N];
+    read_words(p, w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __uint_as_float(w[i]);
+}
+template <int N> __device__ __forceinline__ void read_values(const bf16_t *p, float (&v)[N]) {
+    uint32_t w[N / 2];
+    read_words(p, w);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) { v[i] = __uint_as_float(w[i / 2] << 16); v[i + 1] = __uint_as_float(w[i / 2] & 0xffff0000u); }
+}
+
+// A row of an item: its place among all rows and its head, the positions from .. to - 1 that it is about, and where its result goes.
+struct Row { int b, seq_row0, row, head, from, to; bool whole; size_t slot; };
+
+// The same row from nothing but the positions that it sees, in ordinary fp32 arithmetic: whatever IEEE makes of values that are not finite.  A warp
+// together, a score a lane, then HD / 32 dimensions a lane.  For rows that the matrix instructions cannot do; never on finite inputs.
+template <int HD, typename QT, typename KT, bool PAGED> __device__ __noinline__ void row_by_definition(const Args &a, const Row r) {
+    constexpr int D = HD / 32, N = 16 / (int)sizeof(KT);             // dimensions a lane; values of 16 bytes of a key
+    const int lane = threadIdx.x & 31, kvh = r.head / (a.H / a.KV);
+    const QT *q = static_cast<const QT *>(a.q) + (size_t)r.row * a.q_stride + (size_t)r.head * HD;
+    const KT *kp = static_cast<const KT *>(a.k), *vp = static_cast<const KT *>(a.v) + lane * D;
+    float o[D], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int j = 0; j < D; ++j) o[j] = 0.f;
+#pragma unroll 1
+    for (int p0 = r.from; p0 < r.to; p0 += 32) {
+        size_t k = 0, v = 0;
+        const bool there = p0 + lane < r.to && key_at<HD, PAGED>(a, r.b, r.seq_row0, kvh, p0 + lane, k, v);
+        float s = -INFINITY;
+        if (there) {
+            s = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < HD; i += N) {
+                float x[N], y[N];
+                read_values(q + i, x);
+                read_values(kp + k + i, y);
+#pragma unroll
+                for (int j = 0; j < N; ++j) s = fmaf(x[j], y[j], s);
+            }
+            s *= a.scale_log2;
+        }
+        const unsigned some = __ballot_sync(0xffffffffu, there);
+        const float mn = fmaxf(m, warp_max(s)), base = mn == -INFINITY ? 0.f : mn, f = exp2_approx(m - base), p = there ? exp2_approx(s - base) : 0.f;
+        m = mn;
+        l = l * f + warp_sum(p);
+        bool nan = true;
+#pragma unroll
+        for (int j = 0; j < D; ++j) { o[j] *= f; nan &= o[j] != o[j]; }
+        if (l != l || __all_sync(0xffffffffu, nan)) break;                 // that stays so
+#pragma unroll 8
+        for (int u = 0; u < 32; ++u) {
+            const float pu = __shfl_sync(0xffffffffu, p, u);
+            const size_t vu = __shfl_sync(0xffffffffu, (unsigned long long)v, u);
+            if (!(some >> u & 1)) continue;
+            float y[D];
+            read_values(vp + vu, y);
+#pragma unroll
+            for (int j = 0; j < D; ++j) o[j] = fmaf(pu, y[j], o[j]);
+        }
+    }
+    const float inv = !r.whole ? 1.f : l == 0.f ? 0.f : 1.0f / l;
+    if (!r.whole && lane == 0) a.ml[r.slot] = make_float2(m, l);
+#pragma unroll
+    for (int j = 0; j < D; ++j) {
+        if (!r.whole) a.o[r.slot * HD + lane * D + j] = o[j];
+        else if constexpr (sizeof(QT) == 2) static_cast<QT *>(a.out)[((size_t)r.row * a.H + r.head) * HD + lane * D + j] = float_to_bf16_rne(o[j] * inv);
+        else static_cast<QT *>(a.out)[((size_t)r.row * a.H + r.head) * HD + lane * D + j] = o[j] * inv;
+    }
+}
+
 // Items in parts.  Block (w, j) does eight rows at a time of the item that worker w's run is the first to begin within: the part of worker w - 1
 // and those behind it until the item's end, in their order.  Of few rows each has several of the block's eight warps, which share its parts out;
 // a warp's lanes share the parts' (m, l) out, then hd / 32 dimensions each.  The grid has as many j as the host believes there to be

@@ -251,57 +251,54 @@ struct Job {
     }
 };
 
-// A row whose sums are not finite, where that may have come from a position that it does not see (0 times a V that is not finite): the same
-// from the positions that it does see, one by one.  Positions behind the block's last are zero in the tiles, so only the block's own
-// positions can do it.  Never on finite inputs.
-template <int HD, bool PAGED>
-__device__ __forceinline__ void mend_row(const Args &a, int b, int seq_row0, int from, int tile_end, int kv, int token_row, int head, int last, bool whole, size_t slot) {
-    const int kvh = head / (a.H / a.KV);
-    auto place = [&](int pos, size_t &k, size_t &v) {
-        if (!PAGED) {
-            k = (size_t)(seq_row0 + pos) * a.k_stride + (size_t)kvh * HD;
-            v = (size_t)(seq_row0 + pos) * a.v_stride + (size_t)kvh * HD;
-            return true;
-        }
-        const int idx = pos >> a.page_shift, id = idx < a.max_pages ? a.table[(size_t)b * a.max_pages + idx] : -1;
-        if (id < 0 || id >= a.n_pages) return false;
-        k = v = ((((size_t)id * a.KV + kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1))) * HD;
-        return true;
-    };
-    const bf16_t *kp = static_cast<const bf16_t *>(a.k), *vp = static_cast<const bf16_t *>(a.v);
-    bool disturbed = false;
-    size_t k, v;
-#pragma unroll 1
-    for (int pos = max(last + 1, from); pos < min(tile_end, kv) && !disturbed; ++pos)
-        if (place(pos, k, v)) {
-#pragma unroll 1
-            for (int i = 0; i < HD; ++i) disturbed |= (vp[v + i] & 0x7f80u) == 0x7f80u;
-        }
-    if (!disturbed) return;
-    const bf16_t *q = static_cast<const bf16_t *>(a.q) + (size_t)token_row * a.q_stride + (size_t)head * HD;
-    float o[HD], m = -INFINITY, l = 0.f;
-#pragma unroll 1
-    for (int i = 0; i < HD; ++i) o[i] = 0.f;
-#pragma unroll 1
-    for (int pos = from; pos <= last && pos < tile_end; ++pos) {
-        if (!place(pos, k, v)) continue;
-        float s = 0.f;
-#pragma unroll 1
-        for (int i = 0; i < HD; ++i) s = fmaf(bf16_bits_to_float(q[i]), bf16_bits_to_float(kp[k + i]), s);
-        s *= a.scale_log2;
-        const float mn = fmaxf(m, s), base = mn == -INFINITY ? 0.f : mn, f = exp2_approx(m - base), p = exp2_approx(s - base);
-        m = mn;
-        l = l * f + p;
-#pragma unroll 1
-        for (int i = 0; i < HD; ++i) o[i] = fmaf(p, bf16_bits_to_float(vp[v + i]), o[i] * f);
+// Row rr of half h of an item; token -1: there is none.
+struct Mine {
+    int token, head, last, row, steps;
+    bool whole;
+    __device__ __forceinline__ Mine(const Args &a, const Item<true> &it, const Job &job, int h, int my_token, int my_head) {
+        const int G = a.H / a.KV, v = job.paired ? 2 * it.vh + h : it.vh, kvh = a.subs == 1 ? v : v / a.subs, hh = (a.subs == 1 ? 0 : v % a.subs * a.gs) + my_head;
+        token = my_token + (job.paired ? 0 : h * a.tb);
+        if (my_token < 0 || token >= job.tokens || v >= a.nvh || hh >= G) token = -1;
+        head = kvh * G + hh;
+        last = token >= 0 ? job.seen0 + token : -1;
+        row = it.r.row0 + it.rb * it.r.tb + (token < 0 ? 0 : token);
+        steps = h ? job.n[1] : job.n[0];
+        whole = job.from == 0 && job.to == it.kv;
     }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-#pragma unroll 1
-    for (int i = 0; i < HD; ++i) {
-        if (whole) static_cast<bf16_t *>(a.out)[((size_t)token_row * a.H + head) * HD + i] = float_to_bf16_rne(o[i] * inv);
-        else a.o[slot * HD + i] = o[i];
-    }
-    if (!whole) a.ml[slot] = make_float2(m, l);
+};
+
+// Rows of the block's run whose sums are not finite, where that may have come from a position that they do not see (0 times a V that is not
+// finite): the same by the definition, a row a warp.  Positions behind an item's last are zero in the tiles, so only the item's own new positions can
+// do it.  Never on finite inputs.  It comes behind the block's last item, when no wait is left that could run out meanwhile: 12000 packed tokens with such a V
+// every 64 rows take 170 ms for 0.79, two requests of 120 thousand positions with one each 8.0 for 0.24.
+template <int HD, bool PAGED> __device__ __noinline__ void mend_rows(const Args &a, const Costs<NCOST> &costs, int w, long long x0, long long x1) {
+    constexpr int PIECES = HD / 8;                                   // 16-byte pieces of a position
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    Item<true> it = item_at<true>(a, costs, x0);
+    do {
+        const Job job(a, it, x0, x1);
+        for (int r = warp; r < ROWS; r += warps) {
+            const int h = r / HALF_ROWS, rr = r % HALF_ROWS;
+            const Mine mine(a, it, job, h, rr / a.gs < a.tb ? rr / a.gs : -1, rr % a.gs);
+            if (mine.token < 0 || mine.steps == 0) continue;
+            const size_t slot = ((size_t)w * SLOTS + (job.from > 0 ? 0 : 1)) * ROWS + r;
+            const bf16_t *out = static_cast<const bf16_t *>(a.out) + ((size_t)mine.row * a.H + mine.head) * HD;
+            bool odd = false, disturbed = false;
+            for (int i = lane; i < HD; i += 32) odd |= !isfinite(mine.whole ? bf16_bits_to_float(out[i]) : a.o[slot * HD + i]);
+            if (!__any_sync(0xffffffffu, odd)) continue;
+            const int end = min(min(job.to, job.from + mine.steps * SUB), it.kv), hidden = max(mine.last + 1, job.from);
+            for (int i = lane; i < (end - hidden) * PIECES; i += 32) {
+                size_t k, v;
+                if (!key_at<HD, PAGED>(a, it.b, it.r.row0, mine.head / (a.H / a.KV), hidden + i / PIECES, k, v)) continue;
+                float y[8];
+                read_values(static_cast<const bf16_t *>(a.v) + v + i % PIECES * 8, y);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) disturbed |= !isfinite(y[j]);
+            }
+            if (__any_sync(0xffffffffu, disturbed))
+                row_by_definition<HD, bf16_t, bf16_t, PAGED>(a, Row{it.b, it.r.row0, mine.row, mine.head, job.from, min(mine.last + 1, end), mine.whole, slot});
+        }
+    } while (it.next(a) && it.start < x1);
 }
 
 template <int HD, int MODE>
@@ -313,14 +310,14 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
     __shared__ Costs<NCOST> costs;
     __shared__ uint64_t bars[2 + 2 + 2 * L::TILES + 4 + 4 + 4];        // s_full, p_full and o_full: [half][buffer]
     __shared__ uint32_t tmem_base;
-    __shared__ volatile int quit;
+    __shared__ volatile int quit, odd;                               // a wait gave up; some row is not finite
     __shared__ volatile unsigned info[INFO];                         // the 16-position groups of a step's tile that have a page
     const uint32_t smem = (smem_addr(raw) + 1023u) & ~1023u, q_tile = smem, ring = smem + 2 * L::TILE;
     const uint32_t q_full = smem_addr(bars), q_empty = q_full + 16, kv_full = q_empty + 16, kv_empty = kv_full + 8 * L::TILES, s_full = kv_empty + 8 * L::TILES,
                    p_full = s_full + 32, o_full = p_full + 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        quit = 0;
+        quit = odd = 0;
         for (int i = 0; i < 2; ++i) {
             bar_init(q_full + 8 * i, 1); bar_init(q_empty + 8 * i, 1);
             for (int b = 0; b < 2; ++b) { bar_init(o_full + 8 * (2 * i + b), 1); bar_init(s_full + 8 * (2 * i + b), 2); bar_init(p_full + 8 * (2 * i + b), 4); }
@@ -581,19 +578,14 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
             const int h = warp >> 2, r = h * HALF_ROWS + (warp & 3) * 32 + lane;
             const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), o_at = lanes + O_COL + h * HD;
             unsigned done = 0, step0 = 0;                            // steps of this half
-            const int rr = r % HALF_ROWS, my_head = rr % a.gs, my_token = rr / a.gs < a.tb ? rr / a.gs : -1, G = a.H / a.KV;      // as place_of
+            bool odd_rows = false;                                   // one of this thread's rows is not finite
+            const int rr = r % HALF_ROWS, my_head = rr % a.gs, my_token = rr / a.gs < a.tb ? rr / a.gs : -1;      // as place_of
             while (more && ok) {
                 const Job job(a, it, x0, x1);
-                int token = my_token + (job.paired ? 0 : h * a.tb), head;
-                {
-                    const int v = job.paired ? 2 * it.vh + h : it.vh, kvh = a.subs == 1 ? v : v / a.subs, hh = (a.subs == 1 ? 0 : v % a.subs * a.gs) + my_head;
-                    if (my_token < 0 || token >= job.tokens || v >= a.nvh || hh >= G) token = -1;
-                    head = kvh * G + hh;
-                }
-                const int last = token >= 0 ? job.seen0 + token : -1, first_last = job.seen0 + (job.paired ? 0 : h * a.tb);
-                const int row = (it.r.row0 + it.rb * it.r.tb + (token < 0 ? 0 : token)) * a.H + head;
+                const Mine mine(a, it, job, h, my_token, my_head);
+                const int token = mine.token, last = mine.last, row = mine.row * a.H + mine.head, steps = mine.steps;
+                const int first_last = job.seen0 + (job.paired ? 0 : h * a.tb);
                 const bool live = __any_sync(0xffffffffu, token >= 0);
-                const int steps = h ? job.n[1] : job.n[0];
                 float m = -INFINITY, l = 0.f;
                 for (int u = 0; u < steps && ok; ++u, ++done) {
                     const uint32_t bar = 8 * (2 * h + (done & 1)), s_at = lanes + h * KEYS + (done & 1) * SUB;
@@ -680,7 +672,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 }
                 if (!ok) break;
                 // ---- the rows' ends
-                const bool whole = job.from == 0 && job.to == it.kv;
+                const bool whole = mine.whole;
                 if (steps) {
                     ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a.err, 210);
                     if (!ok) break;
@@ -741,15 +733,13 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                         }
                     }
                     if (token >= 0 && !whole) a.ml[slot + r] = make_float2(m, l);
-                    __syncwarp();
-                    const float odd = bad[0] + bad[1];
-                    if (odd != 0.f && token >= 0)
-                        mend_row<HD, PAGED>(a, it.b, it.r.row0, job.from, min(job.to, job.from + steps * SUB), it.kv, it.r.row0 + it.rb * it.r.tb + token, head, last, whole, slot + r);
+                    odd_rows |= token >= 0 && bad[0] + bad[1] != 0.f;
                     fence_before();
                 }
                 step0 += job.tiles;
                 more = it.next(a) && it.start < x1;
             }
+            if (odd_rows) odd = 1;
         }
         fence_before();
     }
@@ -758,6 +748,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
     }
+    if (odd && !quit) mend_rows<HD, PAGED>(a, costs, w, x0, x1);
 }
 
 }  // namespace tcattn

@@ -111,3 +111,28 @@ def test_scores_far_below_the_largest_weigh_nothing(kb, dtype):
     got = kb.knnssd_packed_attention(q, k, v, start)
     for b in range(8):
         assert (got[9 * b + b:9 * b + 9] == 1.5).all(), f"position {b}"
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_values_that_are_not_finite_in_long_prompts(kb, dtype):
+    """A NaN in one dimension of V every 64 rows: rows before it, in its block too, are finite in that dimension, over all that they see."""
+    lens = [6000, 70, 2500]
+    q, k, v, start = _packed(61, lens, 4, 2, 128, dtype)
+    for b, n in enumerate(lens):
+        for at in range(63, n, 64):
+            v[int(start[b]) + at, 1, at // 64] = (torch.nan, torch.inf, -torch.inf)[at // 64 % 3]
+    got = kb.knnssd_packed_attention(q, k, v, start)
+    for b, n in enumerate(lens):
+        r = slice(int(start[b]), int(start[b]) + n)
+        _check(got[r], *_attend64(q[r], k[r], v[r], torch.ones(n, n, dtype=torch.bool, device="cuda").tril(), 128 ** -0.5), f"prompt {b}")
+
+
+@pytest.mark.parametrize("page", [16, 128])
+def test_values_that_are_not_finite_behind_long_contexts(kb, page):
+    p = Paged(67, [30000, 900, 5000], [40, 3, 130], 2, 128, page, "bf16")
+    for b in (0, 2):
+        at = p.lens[b] + p.fresh[b] - 1
+        p.v[int(p.table[b, at // page]), 0, at % page] = torch.nan
+        p.dense[b][1][at, 0] = torch.nan
+    q = p.q(6, 128, "bf16")
+    _check(p.run(kb, q), *p.want(q))
