@@ -476,6 +476,19 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
                                       int head_dim, const int *row_start_dev, int n_requests, float scale, void *out_dev,
                                       void *cuda_stream);
 
+/*
+ * Whether a bounded wait in an attention call on the current device has given up since this was last asked (it never does in normal
+ * operation): KNNSSD_ERR_TIMEOUT, once, and the rows that were lost by it are NaN.  Only bf16 rows have such waits.  Waits for the stream; calls on
+ * other streams that are still running are not waited for.  KNNSSD_ERR_CUDA while the stream is being captured.
+ */
+knnssd_status knnssd_attention_status(void *cuda_stream);
+
+/*
+ * Test hook: in attention of bf16 rows launched by this process from now on, every block's copies end after `tiles` tiles and waits give up after
+ * spin_limit polls (1 .. 1000000, else KNNSSD_ERR_INVALID_ARG).  spin_limit 0: as before.  Nothing faults or hangs.
+ */
+knnssd_status knnssd_debug_attention_timeout(unsigned spin_limit, unsigned tiles);
+
 #ifdef __cplusplus
 }
 #endif

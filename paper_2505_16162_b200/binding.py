@@ -25,7 +25,8 @@ EXPORTS = ["knnssd_init", "knnssd_destroy", "knnssd_prefill", "knnssd_select_ski
            "knnssd_set_pending", "knnssd_mask_objective", "knnssd_get_stats", "knnssd_last_error", "knnssd_time_pass", "knnssd_trace_pass", "knnssd_linear",
            "knnssd_gemm_split", "knnssd_linear_tc", "knnssd_build_anchors", "knnssd_cosine_top1", "knnssd_cosine_top1_static",
            "knnssd_debug_barrier_timeout", "knnssd_filtered_probs", "knnssd_sample_token", "knnssd_spec_accept",
-           "knnssd_decode_sampled", "knnssd_page_tables", "knnssd_rotary_store", "knnssd_paged_attention", "knnssd_packed_attention"]
+           "knnssd_decode_sampled", "knnssd_page_tables", "knnssd_rotary_store", "knnssd_paged_attention", "knnssd_packed_attention",
+           "knnssd_attention_status", "knnssd_debug_attention_timeout"]
 
 
 class KnnssdError(RuntimeError):
@@ -93,6 +94,8 @@ def _load():
         "knnssd_rotary_store": (I, [P, I, I, L, I, I, I, P, I, P, P, I, I, P, P, P, P, I, P]),
         "knnssd_paged_attention": (I, [P, I, I, L, I, I, I, P, P, I, I, I, P, I, P, P, I, I, F, P, P]),
         "knnssd_packed_attention": (I, [P, P, P, I, I, L, L, L, I, I, I, P, I, F, P, P]),
+        "knnssd_attention_status": (I, [P]),
+        "knnssd_debug_attention_timeout": (I, [C.c_uint, C.c_uint]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -412,6 +415,19 @@ def knnssd_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, r
     _call(_lib.knnssd_packed_attention, "knnssd_packed_attention", dev, qp, kp, vp, dtype, rows, _row_stride(q), _row_stride(k), _row_stride(v), heads,
           k.shape[1], hd, _i32(row_start, B + 1, dev, "row_start"), B, hd ** -0.5 if scale is None else scale, out.data_ptr())
     return out
+
+
+def knnssd_attention_status(device: Optional[int] = None) -> None:
+    """Raises KnnssdError (status 7) if a bounded wait in an attention call on the device (default: the current one) has given up since this was
+    last asked; the rows lost by it are NaN.  Waits for the current stream."""
+    _call(_lib.knnssd_attention_status, "knnssd_attention_status", torch.cuda.current_device() if device is None else device)
+
+
+def knnssd_debug_attention_timeout(spin_limit: int, tiles: int = 0) -> None:
+    """Test hook: attention of bf16 rows loses its copies after `tiles` tiles and gives up after spin_limit polls; 0: as before."""
+    rc = _lib.knnssd_debug_attention_timeout(spin_limit, tiles)
+    if rc:
+        raise KnnssdError(rc, "knnssd_debug_attention_timeout")
 
 
 class Session:

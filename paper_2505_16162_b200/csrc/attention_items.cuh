@@ -34,7 +34,9 @@ struct Args {
     struct Part *parts;
     float2 *ml;
     float *o;
+    // bounded waits (tensor kernel): where one that gives up leaves its code, after how many polls; tiles that a block's copies end after
     int *err;
+    unsigned wait_limit, stop_after;
 };
 
 // first: no run before this one begins within the item; [from, to): the run's positions of it; start: the item (-1: none)

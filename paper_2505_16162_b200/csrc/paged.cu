@@ -7,6 +7,7 @@
 #include "tensor_attention.cuh"
 #include "tensor_maps.cuh"
 
+#include <atomic>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -64,7 +65,7 @@ template <int HD, typename KT, bool PAGED> knnssd_status launch_rows(attn::Args 
     return launched();
 }
 
-// The word that the bounded waits of the tensor-core attention report to: the calls are asynchronous, nothing reads it but a debugger.
+// The word of the current device that the bounded waits of the tensor-core attention report to, until knnssd_attention_status takes it.
 __device__ int g_attention_err;
 int *attention_err_ptr() {
     static int *addr[kMaxDevices] = {};
@@ -74,6 +75,10 @@ int *attention_err_ptr() {
     if (!addr[dev]) cudaGetSymbolAddress(reinterpret_cast<void **>(&addr[dev]), g_attention_err);
     return addr[dev];
 }
+__global__ void take_word_kernel(int *word, int *to) { *to = atomicExch(word, 0); }
+
+// What knnssd_debug_attention_timeout sets: polls of a wait, tiles that a block's copies end after.
+std::atomic<unsigned> g_wait_limit{tcattn::WAIT_LIMIT}, g_stop_after{~0u};
 
 // most_rows: the rows that a request is believed to have at most.
 template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, int most_rows, cudaStream_t s) {
@@ -81,6 +86,7 @@ template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, int most_r
     static bool configured[kMaxDevices] = {};
     const auto kernel = tcattn::tensor_kernel<HD, MODE>;
     a.err = attention_err_ptr();
+    a.wait_limit = g_wait_limit; a.stop_after = g_stop_after;
     if (!a.err || !allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
     const int G = a.H / a.KV, most = tcattn::HALF_ROWS;
     a.gs = (G + (G + most - 1) / most - 1) / ((G + most - 1) / most);
@@ -245,6 +251,33 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
         }
         return head_dim == 128 ? launch_rows<128, float, false>(a, s) : launch_rows<64, float, false>(a, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }
+}
+
+knnssd_status knnssd_attention_status(void *cuda_stream) {
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess || capturing != cudaStreamCaptureStatusNone) {
+        cudaGetLastError();
+        return KNNSSD_ERR_CUDA;
+    }
+    try {
+        int *word = attention_err_ptr(), *taken = nullptr, code = 0;
+        Scratch mem(s);
+        if (!word || !mem.get(&taken, 1)) return KNNSSD_ERR_CUDA;
+        take_word_kernel<<<1, 1, 0, s>>>(word, taken);
+        if (launched() != KNNSSD_OK || cudaMemcpyAsync(&code, taken, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+            cudaGetLastError();
+            return KNNSSD_ERR_CUDA;
+        }
+        return code ? KNNSSD_ERR_TIMEOUT : KNNSSD_OK;
+    } catch (...) { return KNNSSD_ERR_CUDA; }
+}
+
+knnssd_status knnssd_debug_attention_timeout(unsigned spin_limit, unsigned tiles) {
+    if (spin_limit > tcattn::WAIT_LIMIT) return KNNSSD_ERR_INVALID_ARG;
+    g_wait_limit = spin_limit ? spin_limit : tcattn::WAIT_LIMIT;
+    g_stop_after = spin_limit ? tiles : ~0u;
+    return KNNSSD_OK;
 }
 
 }  // extern "C"

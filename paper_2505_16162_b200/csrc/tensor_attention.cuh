@@ -22,7 +22,8 @@
 //   2 requests of 5 rows, 210 000 - 280 000 positions in all  157 / 237 us, 5.6 / 4.9 TB/s: memory, then power
 //   64 requests of 1 row over 2304 positions                 133 / 150 us, 4.6 / 4.1 TB/s: 3.5 items a CTA, 5 - 8 thousand clocks at each one's ends
 //
-// Every wait is bounded; one that gives up sets the error word and all warps leave, after their copies have landed.
+// Every wait is bounded; one that gives up sets the error word, all warps leave after their copies have landed and their products are done, and the rows of the
+// block's run become NaN.
 #pragma once
 
 #include <cuda.h>
@@ -61,21 +62,25 @@ __device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(b), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity, volatile int *quit, int *err, int code) {
+__device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity, volatile int *quit, const Args &a, int code) {
     if (bar_try(b, parity)) return true;
     for (unsigned spins = 0; !bar_try(b, parity);) {
         if (*quit) return false;
-        if (++spins > WAIT_LIMIT) {
+        if (++spins > a.wait_limit) {
             *quit = 1;
-            atomicExch(err, code);
+            atomicExch(a.err, code);
             return false;
         }
     }
     return true;
 }
 // The same for a warp as a whole: all lanes go on, or none.
-__device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int *quit, int *err, int code) {
-    return __all_sync(0xffffffffu, bar_wait(b, parity, quit, err, code));
+__device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int *quit, const Args &a, int code) {
+    return __all_sync(0xffffffffu, bar_wait(b, parity, quit, a, code));
+}
+// For what is on its way and comes whatever else the block does: copies, products.
+__device__ __forceinline__ void bar_settle(uint32_t b, uint32_t parity) {
+    for (unsigned spins = 0; spins < WAIT_LIMIT && !bar_try(b, parity); ++spins) {}
 }
 // One thread of the warp, which goes through them as a whole (a branch on the lane costs some 100 clocks per copy: its operands are moved to
 // uniform registers one by one); `one` is 1 in that thread and 0 in the others.
@@ -301,6 +306,26 @@ template <int HD, bool PAGED> __device__ __noinline__ void mend_rows(const Args 
     } while (it.next(a) && it.start < x1);
 }
 
+// A wait of the block gave up: the rows of its run are NaN, those of cut items by their parts.
+template <int HD> __device__ __noinline__ void spoil_rows(const Args &a, const Costs<NCOST> &costs, int w, long long x0, long long x1) {
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    Item<true> it = item_at<true>(a, costs, x0);
+    do {
+        const Job job(a, it, x0, x1);
+        for (int r = warp; r < ROWS; r += warps) {
+            const int rr = r % HALF_ROWS;
+            const Mine mine(a, it, job, r / HALF_ROWS, rr / a.gs < a.tb ? rr / a.gs : -1, rr % a.gs);
+            if (mine.token < 0 || job.from >= job.to) continue;
+            bf16_t *out = static_cast<bf16_t *>(a.out) + ((size_t)mine.row * a.H + mine.head) * HD;
+            if (!mine.whole) {
+                if (lane == 0) a.ml[((size_t)w * SLOTS + (job.from > 0 ? 0 : 1)) * ROWS + r] = make_float2(0.f, __int_as_float(0x7fffffff));
+            } else {
+                for (int i = lane; i < HD; i += 32) out[i] = 0x7fff;
+            }
+        }
+    } while (it.next(a) && it.start < x1);
+}
+
 template <int HD, int MODE>
 __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                                                         const __grid_constant__ CUtensorMap vmap) {
@@ -308,18 +333,18 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
     constexpr bool PAGED = MODE != PACKED;
     extern __shared__ unsigned char raw[];
     __shared__ Costs<NCOST> costs;
-    __shared__ uint64_t bars[2 + 2 + 2 * L::TILES + 4 + 4 + 4];        // s_full, p_full and o_full: [half][buffer]
+    __shared__ uint64_t bars[2 + 2 + 2 * L::TILES + 4 + 4 + 4 + 2];    // s_full, p_full and o_full: [half][buffer]
     __shared__ uint32_t tmem_base;
     __shared__ volatile int quit, odd;                               // a wait gave up; some row is not finite
     __shared__ volatile unsigned info[INFO];                         // the 16-position groups of a step's tile that have a page
     const uint32_t smem = (smem_addr(raw) + 1023u) & ~1023u, q_tile = smem, ring = smem + 2 * L::TILE;
     const uint32_t q_full = smem_addr(bars), q_empty = q_full + 16, kv_full = q_empty + 16, kv_empty = kv_full + 8 * L::TILES, s_full = kv_empty + 8 * L::TILES,
-                   p_full = s_full + 32, o_full = p_full + 32;
+                   p_full = s_full + 32, o_full = p_full + 32, all_done = o_full + 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         quit = odd = 0;
         for (int i = 0; i < 2; ++i) {
-            bar_init(q_full + 8 * i, 1); bar_init(q_empty + 8 * i, 1);
+            bar_init(q_full + 8 * i, 1); bar_init(q_empty + 8 * i, 1); bar_init(all_done + 8 * i, 1);
             for (int b = 0; b < 2; ++b) { bar_init(o_full + 8 * (2 * i + b), 1); bar_init(s_full + 8 * (2 * i + b), 2); bar_init(p_full + 8 * (2 * i + b), 4); }
         }
         for (int i = 0; i < L::TILES; ++i) { bar_init(kv_full + 8 * i, MODE == COPIED ? LOADERS * 32 + 1 : 1); bar_init(kv_empty + 8 * i, 2); }
@@ -375,9 +400,10 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 if (PAGED && T) { id = page_of(job.j0); next_id = page_of(job.j0 + 1); }
 #pragma unroll 1
                 for (int i = 0; i < total_tiles && ok; ++i) {
+                    if (fills == a.stop_after) { ok = false; break; }          // a test of the waits
                     // half i's q before tile i: the first K is on its way while q waits for the products of the item before
                     if (i < 2 && loader == 0 && (i ? job.n[1] : job.n[0]) > 0) {
-                        ok = warp_wait(q_empty + 8 * i, (qfills[i] & 1) ^ 1, &quit, a.err, 202);
+                        ok = warp_wait(q_empty + 8 * i, (qfills[i] & 1) ^ 1, &quit, a, 202);
                         if (!ok) break;
                         const int vh = job.paired ? 2 * it.vh + i : it.vh, h0 = a.subs == 1 ? vh * a.gs : vh / a.subs * (a.H / a.KV) + vh % a.subs * a.gs;
                         const int row = it.r.row0 + it.rb * it.r.tb + (job.paired ? 0 : i * a.tb);
@@ -400,7 +426,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                         t = i >> 1;
                     }
                     const bool ahead = is_k && t > 0;                // K of the tile behind the one whose V goes by
-                    ok = warp_wait(kv_empty + 8 * slot, (turn_of & 1) ^ 1, &quit, a.err, 201);
+                    ok = warp_wait(kv_empty + 8 * slot, (turn_of & 1) ^ 1, &quit, a, 201);
                     if (!ok) break;
                     const uint32_t dst = ring + slot * L::TILE, bar = kv_full + 8 * slot;
                     const int vh = job.paired ? 2 * it.vh + second : it.vh, kvh = a.subs == 1 ? vh : vh / a.subs;
@@ -467,15 +493,14 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
             // every copy has landed and every product has let go of its tile before the block goes
             for (unsigned i = loader ? fills : fills > L::TILES ? fills - L::TILES : 0; i < fills; ++i) {
                 const unsigned slot = i % L::TILES, parity = i / L::TILES & 1;
-                if (ok) ok = warp_wait(kv_empty + 8 * slot, parity, &quit, a.err, 203);
+                if (ok) ok = warp_wait(kv_empty + 8 * slot, parity, &quit, a, 203);
                 if (MODE != COPIED && !ok)
-                    for (unsigned spins = 0; spins < WAIT_LIMIT && !bar_try(kv_full + 8 * slot, parity); ++spins) {}
+                    bar_settle(kv_full + 8 * slot, parity);
             }
             for (int h = 0; h < 2; ++h)
                 if (qfills[h]) {
-                    if (ok) ok = warp_wait(q_empty + 8 * h, (qfills[h] - 1) & 1, &quit, a.err, 204);
-                    if (!ok)
-                        for (unsigned spins = 0; spins < WAIT_LIMIT && !bar_try(q_full + 8 * h, (qfills[h] - 1) & 1); ++spins) {}
+                    if (ok) ok = warp_wait(q_empty + 8 * h, (qfills[h] - 1) & 1, &quit, a, 204);
+                    if (!ok) bar_settle(q_full + 8 * h, (qfills[h] - 1) & 1);
                 }
         } else if (warp >= MMA_WARP) {
             // ---- products ------------------------------------------------------------------------------------------------
@@ -491,7 +516,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
             // other's tiles out could be a turn of the ring ahead, where a barrier's parity no longer tells one phase from the next.
             unsigned walked = 0;
             auto there = [&]() {
-                if (ok) ok = warp_wait(kv_full + 8 * slot, phase, &quit, a.err, 205);
+                if (ok) ok = warp_wait(kv_full + 8 * slot, phase, &quit, a, 205);
                 if (MODE == COPIED) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // ordinary copies before the products' reads
             };
             auto onward = [&]() {
@@ -546,7 +571,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                     if ((u & 1) || u + 1 == n) commit(k_bar);
                 };
                 if (n > 0) {
-                    if (ok) ok = warp_wait(my_q, q_phase, &quit, a.err, 207);
+                    if (ok) ok = warp_wait(my_q, q_phase, &quit, a, 207);
                     q_phase ^= 1;
                     scores(0);
                     if (n > 1 && ok) scores(1);
@@ -559,7 +584,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                             const unsigned groups = MODE == TILED ? info[(step0 + t) % INFO] : 0xffu;
                             if (MODE != COPIED && ok && (valid < KEYS || groups != 0xffu)) clean(v, valid, groups);
                         }
-                        if (ok) ok = warp_wait(my_p + 8 * vbuf, p_phase, &quit, a.err, 206);
+                        if (ok) ok = warp_wait(my_p + 8 * vbuf, p_phase, &quit, a, 206);
                         if (!ok) break;
                         fence_after();
                         mma_values(o_col, s_col + vbuf * SUB, desc_of(v) + (u & 1) * SUB_STEP, O_DESC, u > 0, my_o + 8 * vbuf);
@@ -573,6 +598,9 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 step0 += T;
                 more = it.next(a) && it.start < x1;
             }
+            // no product of this warp is at work when it leaves, whoever gave up
+            commit(all_done + 8 * h);
+            bar_settle(all_done + 8 * h, 0);
         } else {
             // ---- softmax ---------------------------------------------------------------------------------------------------
             const int h = warp >> 2, r = h * HALF_ROWS + (warp & 3) * 32 + lane;
@@ -590,7 +618,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 for (int u = 0; u < steps && ok; ++u, ++done) {
                     const uint32_t bar = 8 * (2 * h + (done & 1)), s_at = lanes + h * KEYS + (done & 1) * SUB;
                     const int k0 = job.from + u * SUB;
-                    ok = warp_wait(s_full + bar, done >> 1 & 1, &quit, a.err, 208);
+                    ok = warp_wait(s_full + bar, done >> 1 & 1, &quit, a, 208);
                     if (!ok) break;
                     if (!live) {                                     // none of the warp's rows is anyone's: what is in P there stays there
                         __syncwarp();
@@ -626,7 +654,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                         const float f = over ? exp2_approx(m - grown) : 1.f;
                         if (over) { m = grown; l *= f; }
                         if (u > 0) {
-                            ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a.err, 209);
+                            ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a, 209);
                             if (!ok) break;
                             fence_after();
 #pragma unroll 1
@@ -674,7 +702,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 // ---- the rows' ends
                 const bool whole = mine.whole;
                 if (steps) {
-                    ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a.err, 210);
+                    ok = warp_wait(o_full + 8 * (2 * h + (done - 1 & 1)), (done - 1) >> 1 & 1, &quit, a, 210);
                     if (!ok) break;
                     fence_after();
                 }
@@ -748,7 +776,8 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
     }
-    if (odd && !quit) mend_rows<HD, PAGED>(a, costs, w, x0, x1);
+    if (quit) spoil_rows<HD>(a, costs, w, x0, x1);
+    else if (odd) mend_rows<HD, PAGED>(a, costs, w, x0, x1);
 }
 
 }  // namespace tcattn

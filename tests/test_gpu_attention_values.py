@@ -136,3 +136,62 @@ def test_values_that_are_not_finite_behind_long_contexts(kb, page):
         p.dense[b][1][at, 0] = torch.nan
     q = p.q(6, 128, "bf16")
     _check(p.run(kb, q), *p.want(q))
+
+
+# ---- waits that give up ---------------------------------------------------------------------------------------------
+def _stopped(kb, call, tiles):
+    kb.knnssd_debug_attention_timeout(200, tiles)
+    try:
+        got = call()
+        with pytest.raises(kb.KnnssdError) as e:
+            kb.knnssd_attention_status()
+        assert e.value.status == 7
+        kb.knnssd_attention_status()                                 # told once
+    finally:
+        kb.knnssd_debug_attention_timeout(0)
+    return got.double()
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("lens,fresh,KV", [([700], [3], 1), ([30000, 40], [2, 140], 2), ([200] * 90, [1] * 45 + [90] * 45, 4)])
+def test_a_wait_that_gives_up_over_pages(kb, page, lens, fresh, KV):
+    p = Paged(71, lens, fresh, KV, 64, page, "bf16")
+    q = p.q(2 * KV, 64, "bf16")
+    want, tol = p.want(q)
+    kb.knnssd_attention_status()
+    for tiles in (0, 1, 4):
+        got = _stopped(kb, lambda: p.run(kb, q), tiles)
+        lost = got.isnan().any(2)
+        assert got[lost].isnan().all() and (tiles > 0 or lost.all()) and lost.any()
+        _check(got[~lost], want[~lost], tol[~lost], f"rows that were not lost, {tiles} tiles")
+        _check(p.run(kb, q), want, tol, "the call behind it")
+        kb.knnssd_attention_status()
+
+
+def test_a_wait_that_gives_up_in_packed_prompts(kb):
+    lens = [700, 1, 33, 0, 260]
+    q, k, v, start = _packed(73, lens, 4, 2, 128, "bf16")
+    q2, k2, v2 = (torch.cat([x, x[:9]]) for x in (q, k, v))          # rows that no prompt has
+    want = kb.knnssd_packed_attention(q, k, v, start).double()
+    for tiles in (0, 2, 5):
+        got = _stopped(kb, lambda: kb.knnssd_packed_attention(q2, k2, v2, start), tiles)
+        assert got[-9:].abs().max() == 0
+        lost = got[:-9].isnan().any(2)
+        assert lost.any() and got[:-9][lost].isnan().all() and torch.equal(got[:-9][~lost], want[~lost])
+    assert torch.equal(kb.knnssd_packed_attention(q, k, v, start).double(), want)
+
+
+def test_refusals_of_the_hook_and_under_a_capture(kb):
+    with pytest.raises(kb.KnnssdError) as e:
+        kb.knnssd_debug_attention_timeout(1000001)
+    assert e.value.status == 1
+    x = torch.zeros(4, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x += 1
+        with pytest.raises(kb.KnnssdError) as e:
+            kb.knnssd_attention_status()
+        assert e.value.status == 6
+        x += 1
+    graph.replay()
+    assert x.tolist() == [2.0] * 4                                   # the capture has not noticed
