@@ -11,11 +11,12 @@
 //
 // fp32 values are multiplied as three bf16 terms each (24 bits), the products with terms i + j < 3: what an fp32 sum over the rounded inputs
 // gives.  The tensor cores add to a sum by truncation; a sum gets few such additions: the small terms of the scores have a sum of their own, and
-// the 16 positions' share of o is added to it by an ordinary addition.
+// the 16 positions' share of o is added to it by an ordinary addition.  Infinities have no terms: a row whose sums are not finite is done again by the
+// definition, a row at a time (9 prompts of 3001 fp32 tokens in all with an infinite V every 64 rows 0.53 ms for 0.04).
 //
-// Measured: 8 requests of 5 rows and 40 heads over 1280 bf16 positions 56 us, 3.8 TB/s (58 % of a copy's): bound by what a warp issues - the terms, the
+// Measured: 8 requests of 5 rows and 40 heads over 1280 bf16 positions 55 us, 3.8 TB/s (60 % of a copy's): bound by what a warp issues - the terms, the
 // products and the exponentials of 16 positions take the two warps of a scheduler about as long as a copy of them does - and by the ends of items.
-// Two such items of 31 009 positions 40 us, 9 prompts of 3001 fp32 tokens 39.
+// One request of 31 009 positions 40 us, 9 prompts of 3001 fp32 tokens in all 37.
 #pragma once
 
 #include "attention_items.cuh"
@@ -278,25 +279,6 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                         for (int i = 0; i < NQ; ++i) pf[i][2 * h + e] = tm[i];
                     }
                 }
-                // Where the positions are the block's own, a row's p is 0 for those behind it - and 0 times a V that is not finite is not: rows
-                // that see such a position must not disturb the ones that do not.
-                bool odd = false;
-                if (ragged && tokens > 1) {
-                    bool bad = false;
-#pragma unroll 1
-                    for (int i = lane; i < TP * Rg::CHUNKS; i += 32) {
-                        const uint4 v4 = lds16(vb + i * 16);
-                        const uint32_t u[4] = {v4.x, v4.y, v4.z, v4.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            bad |= (u[j] & 0x7f800000u) == 0x7f800000u;
-                            if (NK == 1) bad |= (u[j] & 0x7f80u) == 0x7f80u;
-                        }
-                    }
-                    odd = __any_sync(0xffffffffu, bad);
-                }
-                // o[n][2 e + i] is dimension col(n, i) of row 8 e + g
-                auto col = [&](int n, int i) { return NK == 1 ? 8 * n + 2 * t + i : 32 * (n >> 2) + 4 * (2 * t + i) + (n & 3); };
                 auto products = [&](int n, const uint32_t (&b0)[2][NK], const uint32_t (&b1)[2][NK]) {       // of 16 dimensions: tiles n and n + 1
                     float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -310,41 +292,7 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
 #pragma unroll
                         for (int i = 0; i < 4; ++i) o[n + u][i] += d[u][i];
                 };
-                if (odd) {                                           // position by position, into the rows that see it
-#pragma unroll 1
-                    for (int q = 0; q < TP && p + q < it.kv; ++q) {
-                        const int reg = 2 * (q >> 3), from_lane = (lane & ~3) + ((q & 7) >> 1);
-                        float pq[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float v = 0.f;
-#pragma unroll
-                            for (int i = 0; i < NQ; ++i) {
-                                const uint32_t u = reg ? pf[i][2 + e] : pf[i][e];
-                                v += __uint_as_float(q & 1 ? u & 0xffff0000u : u << 16);
-                            }
-                            pq[e] = __shfl_sync(0xffffffffu, v, from_lane);
-                        }
-#pragma unroll
-                        for (int n = 0; n < NTILE; ++n)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int d = col(n, i), piece = d * (int)sizeof(KT) / 16, in_piece = d * (int)sizeof(KT) % 16;
-                                const uint32_t addr = vb + q * Rg::ROW + Rg::vswz(q, piece) * 16 + in_piece;
-                                float v;
-                                if constexpr (NK == 1) {
-                                    unsigned short u;
-                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(addr));
-                                    v = bf16_bits_to_float(u);
-                                } else {
-                                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-                                }
-#pragma unroll
-                                for (int e = 0; e < 2; ++e)
-                                    if (p + q <= last[e]) o[n][2 * e + i] = fmaf(pq[e], v, o[n][2 * e + i]);
-                            }
-                    }
-                } else if constexpr (NK == 1) {
+                if constexpr (NK == 1) {
 #pragma unroll
                     for (int n2 = 0; n2 < NTILE / 2; ++n2) {         // matrices: positions 0..7 and 8..15 of 8 dimensions, then of the next 8
                         uint32_t r[4];
@@ -379,11 +327,19 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                 if (++stage == Rg::STAGES) stage = 0;
             }
             // ---- the rows' ends ----------------------------------------------------------------------------------------
+            // o[n][2 e + i] is dimension col(n, i) of row 8 e + g
             auto col = [&](int n, int i) { return NK == 1 ? 8 * n + 2 * t + i : 32 * (n >> 2) + 4 * (2 * t + i) + (n & 3); };
             const bool whole = from == 0 && to == it.kv;
             const size_t slot = ((size_t)w * SLOTS + (from > 0 ? 0 : 1)) * 16;
+            unsigned odd[2];                                         // lanes with a sum of row 8 e + g that is not finite
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
+                float bad[2] = {0.f, 0.f};                           // 0 times the sums: not 0 where one is not finite
+#pragma unroll
+                for (int n = 0; n < NTILE; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) bad[i] = fmaf(o[n][2 * e + i], 0.f, bad[i]);
+                odd[e] = __ballot_sync(0xffffffffu, bad[0] + bad[1] != 0.f);
                 float ls = l[e];
                 ls += __shfl_xor_sync(0xffffffffu, ls, 1);
                 ls += __shfl_xor_sync(0xffffffffu, ls, 2);
@@ -401,6 +357,14 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                         d[col(n, 1)] = o[n][2 * e + 1] * f;
                     }
                 }
+            }
+            // Such a row may be so only by the products: 0 times a V that is not finite and that the row does not see, an infinity (or a value that bf16 rounds
+            // to one) in three terms.
+            if (odd[0] | odd[1]) {
+                __syncwarp();                                        // behind the other lanes' stores
+                for (int r = 0; r < live; ++r)
+                    if (odd[r >> 3] >> (4 * (r & 7)) & 15u)
+                        row_by_definition<HD, float, KT, PAGED>(a, Row{it.b, it.r.row0, row0 + r / heads, h0 + r % heads, from, min(seen0 + r / heads + 1, to), whole, slot + r});
             }
         }
         any = it.next(a) && it.start < x1;

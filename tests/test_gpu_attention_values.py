@@ -195,3 +195,67 @@ def test_refusals_of_the_hook_and_under_a_capture(kb):
         x += 1
     graph.replay()
     assert x.tolist() == [2.0] * 4                                   # the capture has not noticed
+
+
+# ---- fp32 rows: infinities, and values near the type's largest ----------------------------------------------------------
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("cache", ["fp32", "bf16"])
+@pytest.mark.parametrize("lens,first", [(20, 0), (300, 128)])
+def test_keys_that_are_not_finite_fp32(kb, value, cache, lens, first):
+    p = Paged(79, [lens] * 16, [6] * 16, 2, 64, 16, cache)
+    for b in range(16):
+        at = first + b
+        p.k[int(p.table[b, at // 16]), 1, at % 16, 7] = value
+        p.dense[b][0][at, 1, 7] = value
+    q = p.q(4, 64, "fp32")
+    got = p.run(kb, q)
+    for b in range(16):
+        r = slice(6 * b, 6 * b + 6)
+        want, tol = _by_scores(q[r], *p.dense[b], p.seen(b), 64 ** -0.5)
+        assert want.isnan().any() and not want.isnan().all()
+        _check(got[r], want, tol, f"position {first + b}")
+
+
+@pytest.mark.parametrize("dtype,cache", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("lens,fresh", [([50, 40], [4, 1]), ([30000, 10], [2, 20])])
+def test_an_infinite_value_that_is_seen_is_the_result(kb, dtype, cache, lens, fresh):
+    p = Paged(83, lens, fresh, 1, 128, 16, cache)
+    for b, at, d, val in ((0, 17, 3, torch.inf), (0, 18, 9, -torch.inf), (1, lens[1] + fresh[1] - 1, 100, torch.inf)):
+        p.v[int(p.table[b, at // 16]), 0, at % 16, d] = val
+        p.dense[b][1][at, 0, d] = val
+    q = p.q(4, 128, dtype)
+    want, tol = p.want(q)
+    for b, at, d, val in ((0, 17, 3, torch.inf), (0, 18, 9, -torch.inf), (1, lens[1] + fresh[1] - 1, 100, torch.inf)):
+        r = torch.arange(p.rows, device="cuda")
+        sees = (r >= p.start[b]) & (r < p.start[b + 1]) & (lens[b] + r - p.start[b] >= at)
+        want[sees, :, d] = val
+    got = p.run(kb, q).double()
+    inf = want.isinf()
+    assert torch.equal(got[inf], want[inf])
+    _check(got[~inf], want[~inf], tol[~inf])
+
+
+@pytest.mark.parametrize("what", ["fp32 over pages", "packed"])
+def test_the_largest_values_that_are_not_seen_fp32(kb, what):
+    """V of the type's largest: rounded to bf16, as the first of three terms, it is infinite."""
+    most = torch.finfo(torch.float32).max
+    lens = [37] * 16
+    if what == "packed":
+        q, k, v, start = _packed(89, lens, 4, 2, 64, "fp32")
+        for b in range(16):
+            v[37 * b + 20 + b] = most
+        got = kb.knnssd_packed_attention(q, k, v, start)
+        for b in range(16):
+            r = slice(37 * b, 37 * b + 20 + b)
+            n = 20 + b
+            _check(got[r], *_attend64(q[r], k[r], v[r], torch.ones(n, n, dtype=torch.bool, device="cuda").tril(), 64 ** -0.5), f"prompt {b}")
+        return
+    p = Paged(97, [60 + b for b in range(16)], [4] * 16, 2, 64, 16, "fp32")
+    for b in range(16):
+        at = p.lens[b] + 3
+        p.v[int(p.table[b, at // 16]), :, at % 16] = -most
+    q = p.q(4, 64, "fp32")
+    got = p.run(kb, q)
+    for b in range(16):
+        r = slice(4 * b, 4 * b + 3)
+        _check(got[r], *_attend64(q[r], p.dense[b][0][:-1], p.dense[b][1][:-1], p.seen(b)[:3, :-1], 64 ** -0.5), f"request {b}")
