@@ -453,8 +453,8 @@ knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, lo
  *              (negative: KNNSSD_ERR_INVALID_ARG)
  *   scale      finite and not negative, else KNNSSD_ERR_INVALID_ARG; 0 gives equal weights
  *   n_rows * n_heads below 2^31, else KNNSSD_ERR_CAPACITY
- * Positions whose page id is outside [0, n_pages) are not seen; a row that sees nothing gives zeros, and so do rows at and behind
- * row_start[n_requests].  What a row does not see never reaches it, not even NaN.  fp32 rows: 24-bit products, fp32 sums; bf16 rows: the softmax
+ * Positions whose page id is outside [0, n_pages) are not seen; a row that sees nothing gives zeros, and so do rows before row_start[0] and from
+ * row_start[n_requests] on.  What a row does not see never reaches it, not even NaN.  fp32 rows: 24-bit products, fp32 sums; bf16 rows: the softmax
  * weights are rounded to bf16 for the product with V.  Runs of positions that go to one warp follow from all lengths of the call: a row's
  * last bits depend on the company it has, not on chance.
  */
@@ -469,7 +469,7 @@ knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, l
  * row_start[b] + i.  Prompts may be empty.
  *   q_dev, k_dev, v_dev  DEVICE [n_rows][heads][head_dim] of one type, rows *_stride elements apart (views of one map's output serve)
  *   out_dev              DEVICE [n_rows][n_heads][head_dim], same type
- * Scale, limits, rounding, empty rows and rows behind the last prompt as in knnssd_paged_attention.
+ * Scale, limits, rounding, empty rows and rows that no prompt has as in knnssd_paged_attention.
  */
 knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, const void *v_dev, int dtype, int n_rows,
                                       long long q_stride, long long k_stride, long long v_stride, int n_heads, int n_kv_heads,

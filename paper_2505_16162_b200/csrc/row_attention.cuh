@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     sum_costs<false>(a, costs);
-    clear_tail<float>(a, HD, blockIdx.x * NT + threadIdx.x, gridDim.x * NT);
+    clear_others<float>(a, HD, blockIdx.x * NT + threadIdx.x, gridDim.x * NT);
     const long long total = costs.pfx[NT];
     const int W = workers_of(a, total);
     // neighbouring runs go to different SMs: a short launch spreads over the chip

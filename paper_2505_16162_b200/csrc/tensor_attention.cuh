@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
     sum_costs<true>(a, costs);                                       // has the block's barriers
     fence_after();
     const uint32_t tmem = tmem_base;
-    clear_tail<bf16_t>(a, HD, blockIdx.x * blockDim.x + tid, gridDim.x * blockDim.x);
+    clear_others<bf16_t>(a, HD, blockIdx.x * blockDim.x + tid, gridDim.x * blockDim.x);
     const long long total = costs.pfx[NCOST];
     const int w = blockIdx.x, W = total > 0 ? workers_of(a, total) : 0;
     const long long x0 = w < W ? run_start(total, w, W) : 0, x1 = w < W ? run_start(total, w + 1, W) : 0;

@@ -259,3 +259,16 @@ def test_the_largest_values_that_are_not_seen_fp32(kb, what):
     for b in range(16):
         r = slice(4 * b, 4 * b + 3)
         _check(got[r], *_attend64(q[r], p.dense[b][0][:-1], p.dense[b][1][:-1], p.seen(b)[:3, :-1], 64 ** -0.5), f"request {b}")
+
+
+# ---- rows that no request has -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("start", [[5, 70, 100], [130, 130, 130], [0, 0, 0], [7, 7, 40]])
+def test_rows_before_the_first_request(kb, dtype, start):
+    q, k, v, _ = _packed(101, [130], 4, 2, 64, dtype)
+    out = torch.full((130, 4, 64), torch.nan, device="cuda", dtype=q.dtype)
+    kb.knnssd_packed_attention(q, k, v, torch.tensor(start, dtype=torch.int32, device="cuda"), out=out)
+    for a, b in zip(start, start[1:]):
+        if b > a:
+            _check(out[a:b], *_attend64(q[a:b], k[a:b], v[a:b], torch.ones(b - a, b - a, dtype=torch.bool, device="cuda").tril(), 64 ** -0.5))
+    assert not out[:start[0]].any() and not out[start[-1]:].any()
