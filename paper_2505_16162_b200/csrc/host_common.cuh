@@ -17,6 +17,15 @@ namespace knnssd {
 // 64, knnssd_gemm_split over 5120 x 13824 weights mapped memory on every call (77 rows 336 us, with 96 129; 1024 rows 488, 275).
 constexpr unsigned long long kPoolKeep = 96ull << 20;
 
+// What a call sets up once (pools, addresses, attributes) is no part of a capture that its thread may be in: within this, such calls are let through
+// rather than end it.
+struct ApartFromCapture {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    ApartFromCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    ~ApartFromCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    ApartFromCapture(const ApartFromCapture &) = delete;
+};
+
 struct DevicePools {
     std::mutex mu;
     cudaMemPool_t pool[64] = {};
@@ -28,6 +37,7 @@ struct DevicePools {
         std::lock_guard<std::mutex> lock(mu);
         if (!tried[dev]) {
             tried[dev] = true;
+            const ApartFromCapture apart;
             int has = 0;
             cudaMemPoolProps props{};
             props.allocType = cudaMemAllocationTypePinned;

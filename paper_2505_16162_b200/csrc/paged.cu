@@ -25,6 +25,7 @@ knnssd_status launched() { return cudaGetLastError() == cudaSuccess ? KNNSSD_OK 
 template <typename K> bool allow_smem(K kernel, int bytes, bool (&done)[kMaxDevices]) {
     const int dev = current_device_slot();
     if (done[dev]) return true;
+    const ApartFromCapture apart;
     done[dev] = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
     return done[dev];
 }
@@ -72,7 +73,10 @@ int *attention_err_ptr() {
     static std::mutex mu;
     const int dev = current_device_slot();
     std::lock_guard<std::mutex> lock(mu);
-    if (!addr[dev]) cudaGetSymbolAddress(reinterpret_cast<void **>(&addr[dev]), g_attention_err);
+    if (!addr[dev]) {
+        const ApartFromCapture apart;
+        cudaGetSymbolAddress(reinterpret_cast<void **>(&addr[dev]), g_attention_err);
+    }
     return addr[dev];
 }
 __global__ void take_word_kernel(int *word, int *to) { *to = atomicExch(word, 0); }
