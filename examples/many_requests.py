@@ -71,6 +71,7 @@ class Batch:
                     k = torch.empty(len(tokens), sh.n_kv_heads, sh.head_dim, device="cuda")
                     q = kb.knnssd_rotary_store(qkv, self.cos_sin, s["pos"], s["slot"], k_pages, v_pages, k_rows=k)
                     v = qkv.view(len(tokens), -1, sh.head_dim)[:, -sh.n_kv_heads:]
+                    k, v = (t.to(k_pages.dtype).float() for t in (k, v))             # what later passes read from the pages
                     o = kb.knnssd_packed_attention(q, k, v, s["start"])
                 else:
                     q = kb.knnssd_rotary_store(qkv, self.cos_sin, s["pos"], s["slot"], k_pages, v_pages)
