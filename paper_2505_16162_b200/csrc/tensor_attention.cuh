@@ -62,17 +62,21 @@ __device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(b), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity, volatile int *quit, const Args &a, int code) {
-    if (bar_try(b, parity)) return true;
+// The polls are a piece of code of their own: the warps' loops, each its own way through the kernel, are shorter for it (12000 packed tokens 703 us with them in
+// every wait, 682 so).
+static __device__ __noinline__ bool bar_poll(uint32_t b, uint32_t parity, volatile int *quit, unsigned limit, int *err, int code) {
     for (unsigned spins = 0; !bar_try(b, parity);) {
         if (*quit) return false;
-        if (++spins > a.wait_limit) {
+        if (++spins > limit) {
             *quit = 1;
-            atomicExch(a.err, code);
+            atomicExch(err, code);
             return false;
         }
     }
     return true;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity, volatile int *quit, const Args &a, int code) {
+    return bar_try(b, parity) || bar_poll(b, parity, quit, a.wait_limit, a.err, code);
 }
 // The same for a warp as a whole: all lanes go on, or none.
 __device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int *quit, const Args &a, int code) {
@@ -186,11 +190,6 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     uint64_t d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -202,20 +201,24 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// 2^x of two values on the multiply-add units: x = n + f with n the nearest whole number (added to 1.5 2^23 + 127 it is the sum's low bits, biased as
-// an exponent is), 2^f by a cubic (minimax of the relative error on [-1/2, 1/2] by Lawson's weighted least squares: 7.5e-5, a fiftieth of what
-// rounding to bf16 does at most), times 2^n.  n = -127 stands for 0, so that what a row does not see has no weight at all; NaN gives 0 as well.
+// 2^x of two values on the multiply-add units: x = n + f with n the nearest whole number (added to 1.5 2^23 it is the sum's low bits), 2^f by a
+// cubic (minimax of the relative error on [-1/2, 1/2] by Lawson's weighted least squares: 7.5e-5, a fiftieth of what rounding to bf16
+// does at most), and n added to the exponent.  At x = -126.999 the exponent ends at 0 and what is left, 6e-4 2^-126, is 0 as bf16: below that, and for what a
+// row does not see, there is no weight at all.  (With 2^n as a factor instead, 0 for n = -127, packed prompts and long contexts take 1 % longer.)  NaN gives 0
+// as well.
 __device__ __forceinline__ void exp2_cubic(uint64_t x, float &a, float &b) {
     float x0, x1;
     split(x, x0, x1);
-    x = pair_of(fmaxf(x0, -127.f), fmaxf(x1, -127.f));
-    const uint64_t n = add2(x, pair_of(12583039.f, 12583039.f)), f = fma2(add2(n, pair_of(-12583039.f, -12583039.f)), pair_of(-1.f, -1.f), x);
+    x = pair_of(fmaxf(x0, -126.999f), fmaxf(x1, -126.999f));
+    const uint64_t n = add2(x, pair_of(12582912.f, 12582912.f)), f = fma2(add2(n, pair_of(-12582912.f, -12582912.f)), pair_of(-1.f, -1.f), x);
     uint64_t y = fma2(f, pair_of(0.0551716685295105f, 0.0551716685295105f), pair_of(0.2426111251115799f, 0.2426111251115799f));
     y = fma2(f, y, pair_of(0.6932609677314758f, 0.6932609677314758f));
     y = fma2(f, y, pair_of(0.9999280571937561f, 0.9999280571937561f));
-    float n0, n1;
+    float y0, y1, n0, n1;
+    split(y, y0, y1);
     split(n, n0, n1);
-    split(mul2(y, pair_of(__float_as_uint(n0) << 23, __float_as_uint(n1) << 23)), a, b);
+    a = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(n0) << 23));
+    b = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(n1) << 23));
 }
 
 // Lane 4 i + j has row j of a 4 x 4 square of 16-byte pieces; afterwards it has column j.
@@ -398,9 +401,9 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 const bool own = job.paired && job.n[0] > 0 && job.n[1] > 0;
                 const int T = job.tiles, total_tiles = (own ? 4 : 2) * T;
                 if (PAGED && T) { id = page_of(job.j0); next_id = page_of(job.j0 + 1); }
+                const int until = (int)min((unsigned)total_tiles, a.stop_after - fills);      // fewer in a test of the waits alone
 #pragma unroll 1
-                for (int i = 0; i < total_tiles && ok; ++i) {
-                    if (fills == a.stop_after) { ok = false; break; }          // a test of the waits
+                for (int i = 0; i < until && ok; ++i) {
                     // half i's q before tile i: the first K is on its way while q waits for the products of the item before
                     if (i < 2 && loader == 0 && (i ? job.n[1] : job.n[0]) > 0) {
                         ok = warp_wait(q_empty + 8 * i, (qfills[i] & 1) ^ 1, &quit, a, 202);
@@ -486,6 +489,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                     ++fills;
                     if (++slot == L::TILES) { slot = 0; ++turn_of; }
                 }
+                ok &= until == total_tiles;
                 step0 += T;
                 more = it.next(a) && it.start < x1;
             }
