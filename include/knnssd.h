@@ -454,9 +454,13 @@ knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, lo
  *   scale      finite and not negative, else KNNSSD_ERR_INVALID_ARG; 0 gives equal weights
  *   n_rows * n_heads below 2^31, else KNNSSD_ERR_CAPACITY
  * Positions whose page id is outside [0, n_pages) are not seen; a row that sees nothing gives zeros, and so do rows before row_start[0] and from
- * row_start[n_requests] on.  What a row does not see never reaches it, not even NaN.  fp32 rows: 24-bit products, fp32 sums; bf16 rows: the softmax
- * weights are rounded to bf16 for the product with V.  Runs of positions that go to one warp follow from all lengths of the call: a row's
- * last bits depend on the company it has, not on chance.
+ * row_start[n_requests] on.  What a row does not see never reaches it, not even NaN; what it sees and is not finite counts as in IEEE arithmetic (a score of
+ * NaN or +inf makes the row NaN, one of -inf has no weight).  Such calls are slower, up to some hundred times.  Values so large that a sum of weights times
+ * V, before it is divided by the sum of weights, passes fp32's range give an infinity.
+ * fp32 rows: 24-bit products, fp32 sums.  bf16 rows: the softmax weights are rounded to bf16 for the product with V, a quarter of their powers of two are good
+ * to 7.5e-5, and the tensor cores' sums in fp32 round towards zero; with the result's own rounding 1.8e-3 .. 2.3e-3 relative (root of the mean square), where that
+ * rounding alone is 1.7e-3.  Runs of positions that go to one warp follow from all lengths of the call: a row's last bits depend on the company it has, not on
+ * chance.
  */
 knnssd_status knnssd_paged_attention(const void *q_dev, int dtype, int n_rows, long long q_stride, int n_heads,
                                      int n_kv_heads, int head_dim, const void *k_pages_dev, const void *v_pages_dev,

@@ -165,9 +165,10 @@ template <int TP, bool HALVES> __device__ __forceinline__ void note_part(const A
 
 // Rows before the first request's and behind the last one's are nobody's: zeros.
 template <typename T> __device__ __forceinline__ void clear_others(const Args &a, int hd, int thread, int threads) {
-    const long long row = (long long)a.H * hd, first = min(max(a.row_start[0], 0), a.R), used = min(max(a.row_start[a.B], 0), a.R);
-    for (long long i = thread; i < first * row; i += threads) static_cast<T *>(a.out)[i] = T(0);
-    for (long long i = max(first, used) * row + thread; i < a.R * row; i += threads) static_cast<T *>(a.out)[i] = T(0);
+    const int first = min(max(a.row_start[0], 0), a.R), used = max(first, min(a.row_start[a.B], a.R)), others = first + a.R - used;
+    if (others == 0) return;
+    const long long row = (long long)a.H * hd, held = (used - first) * row;
+    for (long long i = thread; i < others * row; i += threads) static_cast<T *>(a.out)[i < first * row ? i : i + held] = T(0);
 }
 
 // Row r of an item's rows (ROWS, two halves of ROWS / 2 where HALVES): the new row of the block and the query head; -1 where there is none.

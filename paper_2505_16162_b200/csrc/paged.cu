@@ -55,8 +55,10 @@ template <int HD, typename KT, bool PAGED> knnssd_status launch_rows(attn::Args 
     // of 5 new rows 56 / 58 / 66; least_run 16 / 32 / 64 / 256: 2 requests of 1851 positions 33 / 24 / 22 / -, one of 96 15 / 15 / 15 / 29.
     a.extra = 64;
     a.least_run = 64;
-    // Parts an item may be in, as the merge takes them 32 at a time: at most 32 / 64 / 128 / any number (296): one request of 31 009 positions 85 / 51 / 40 /
-    // 56 us, two of 74 011 205 / 119 / 87 / 105.
+    // Parts an item may be in, on average over the call's items, as the merge takes them 32 at a time: at most 32 / 64 / 128 / any number (296): one request
+    // of 31 009 positions 85 / 51 / 40 / 56 us, two of 74 011 205 / 119 / 87 / 105.  A long item beside short ones is in more, up to all workers: 31 009
+    // positions and 40 times 100, 8 heads on one of K/V, 85 us for 41 alone; 4 heads of their own 31 for 35.  A bound by the longest item instead (41, 41)
+    // cost short prompts 4 % for the search.
     const int ctas = sm_count();
     a.most = (int)std::min((long long)ctas * Rg::WARPS, 128ll * a.nvh * std::max(a.B, a.R / a.tb));
     Scratch mem(s);
