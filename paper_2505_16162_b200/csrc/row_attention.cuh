@@ -16,7 +16,7 @@
 //
 // Measured: 8 requests of 5 rows and 40 heads over 1280 bf16 positions 55 us, 3.8 TB/s (60 % of a copy's): bound by what a warp issues - the terms, the
 // products and the exponentials of 16 positions take the two warps of a scheduler about as long as a copy of them does - and by the ends of items.
-// One request of 31 009 positions 40 us, 9 prompts of 3001 fp32 tokens in all 37.
+// One request of 31 009 positions 40 us, 9 prompts of 3001 fp32 tokens in all 38.
 #pragma once
 
 #include "attention_items.cuh"

@@ -17,10 +17,13 @@
 // Both halves share the K/V tiles; where a request has no more rows than one half, the halves are two K/V heads with tiles of their own.
 //
 // Measured, in a row of calls from a cool start / for seconds on end, when the chip runs at its power limit (1.6 - 1.7 GHz):
-//   12000 packed tokens in 4 prompts, 40 heads (8 of K/V)    725 / 840 us, 1.05 / 0.90 PFLOP/s: the exponentials (8 clocks a warp for each value
+//   12000 packed tokens in 4 prompts, 40 heads (8 of K/V)    680 / 792 us, 1.12 / 0.96 PFLOP/s: the exponentials (8 clocks a warp for each value
 //                                                           of its rows) and what stands beside them in the softmax, then power
-//   2 requests of 5 rows, 210 000 - 280 000 positions in all  157 / 237 us, 5.6 / 4.9 TB/s: memory, then power
-//   64 requests of 1 row over 2304 positions                 133 / 150 us, 4.6 / 4.1 TB/s: 3.5 items a CTA, 5 - 8 thousand clocks at each one's ends
+//   2 requests of 5 rows, 210 000 - 300 000 positions in all  159 / 238 us, 5.5 / 4.8 TB/s: memory, then power
+//   64 requests of 1 row over 2304 positions                 134 / 149 us, 4.6 / 4.1 TB/s: 3.5 items a CTA, 5 - 8 thousand clocks at each one's ends
+//
+// Fewer bits: P is rounded to bf16 (2^-8 relative at most), as the products take it, a quarter of it comes from a cubic of 7.5e-5, and O's sums in tensor memory
+// round towards zero.  Against 64 bits, with the result's own rounding, 1.8e-3 .. 2.3e-3 for 1.7e-3 by that rounding alone.
 //
 // Every wait is bounded; one that gives up sets the error word, all warps leave after their copies have landed and their products are done, and the rows of the
 // block's run become NaN.
