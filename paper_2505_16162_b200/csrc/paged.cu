@@ -101,9 +101,9 @@ template <int HD, int MODE> knnssd_status launch_tensor(attn::Args a, int most_r
     a.tb = most / a.gs;
     const int ctas = sm_count();
     // An item's beginning and end cost a CTA some 5 to 8 thousand clocks, as much as these positions: with 0 / 384 / 1024, 24 short prompts take
-    // 89 / 35 / 34 us and 12000 tokens in 4 prompts 943 / 729 / 776.
+    // 88 / 34 / 33 us and 12000 tokens in 4 prompts 935 / 709 / 750.
     a.extra = 384;
-    // What a CTA takes at least: with 64 / 512 / 2048, 6 requests of 13 thousand positions take 33 / 32 / 42 us, 24 short prompts 35 / 35 / 40.
+    // What a CTA takes at least: with 64 / 512 / 2048, 6 requests of 13 thousand positions take 33 / 32 / 42 us, 24 short prompts 34 / 34 / 39.
     a.least_run = 512;
     // Two heads a block where there are items enough for all CTAs either way: half as many beginnings and ends, half as many pieces.  1440 items
     // of one row 44 -> 33 us, 768 of about 100 rows 43 -> 35, 512 of one row and 200 positions 46 -> 43; but 16 of 35 thousand positions 35 -> 45,

@@ -17,7 +17,7 @@
 // Both halves share the K/V tiles; where a request has no more rows than one half, the halves are two K/V heads with tiles of their own.
 //
 // Measured, in a row of calls from a cool start / for seconds on end, when the chip runs at its power limit (1.6 - 1.7 GHz):
-//   12000 packed tokens in 4 prompts, 40 heads (8 of K/V)    680 / 792 us, 1.12 / 0.96 PFLOP/s: the exponentials (8 clocks a warp for each value
+//   12000 packed tokens in 4 prompts, 40 heads (8 of K/V)    680 - 710 / 792 us, 1.1 / 0.96 PFLOP/s: the exponentials (8 clocks a warp for each value
 //                                                           of its rows) and what stands beside them in the softmax, then power
 //   2 requests of 5 rows, 210 000 - 300 000 positions in all  159 / 238 us, 5.5 / 4.8 TB/s: memory, then power
 //   64 requests of 1 row over 2304 positions                 134 / 149 us, 4.6 / 4.1 TB/s: 3.5 items a CTA, 5 - 8 thousand clocks at each one's ends
@@ -46,8 +46,8 @@ constexpr int BAND = KEYS * 128;          // bytes of 64 dimensions of a tile: r
 constexpr int INFO = 16;                  // steps whose page masks are kept
 constexpr unsigned WAIT_LIMIT = 1000000u;
 constexpr float GROWTH = 8.f;
-// One pair in four takes its powers of two from the multiply-add units (a cubic, below): with none, one in eight, three in eight 12000 packed tokens take
-// as long or longer.  8 clocks a warp's ex2 against 3.2 for a packed multiply-add.
+// One pair in four takes its powers of two from the multiply-add units (a cubic, below): with none / one in eight / one in four / three in eight 12000 packed
+// tokens take 750 / 739 / 709 / 726 us.  8 clocks a warp's ex2 against 3.2 for a packed multiply-add.
 constexpr int CUBIC = 1, CUBIC_OF = 4;
 constexpr int TMEM_COLS = 512, O_COL = 256;
 
