@@ -493,6 +493,79 @@ knnssd_status knnssd_attention_status(void *cuda_stream);
  */
 knnssd_status knnssd_debug_attention_timeout(unsigned spin_limit, unsigned tiles);
 
+/* ---- drafts that branch ----
+ *
+ * A request's new rows may be a tree of tokens: row 0 is the pending token, row i > 0 a drafted token that follows the row row_parent[i] < i of the same request.
+ * Siblings are tested in row order.  Rows, requests, pages and slots are those of the calls above: knnssd_page_tables gives row i the slot of position lens[b] + i,
+ * knnssd_tree_tables the position that its embedding is rotated by (knnssd_rotary_store's row_pos) and the word of what it sees.  After the attention of all layers
+ * knnssd_tree_accept (sampled) or knnssd_tree_agree (greedy) finds the rows that are kept, knnssd_keep_rows moves their K and V behind the lens[b] positions held, and
+ * the request is n_accepted + 1 positions longer.  All calls are asynchronous on the stream and may be captured; none needs scratch except the attention.
+ * row_start [n_requests + 1] gives a request its rows; rows that no request has (before row_start[0], from row_start[n_requests] on) may be there.
+ */
+
+/*
+ * Positions and words of the rows.  Bit d (0 .. 63) of row i's word says whether it sees position lens[b] + i - d; positions 64 and more before its own are always
+ * seen.  Set are the bits of the row itself (d = 0), of the rows that it follows, directly or not, and of all that lies before the request's new rows.  The words are
+ * relative to the row's own slot: they hold as well for calls of knnssd_tree_attention on some of the rows (a tree drafted level by level, lens[b] then counting the rows before).
+ *   row_parent_dev [n_rows]   in: -1 .. i - 1 for row i of its request; -1: it follows what the request holds
+ *   row_pos_dev [n_rows]      out: lens[b] and the number of rows that it follows; may be the array that knnssd_page_tables filled
+ *   row_seen_dev [n_rows]     out: words, 8-byte aligned (else KNNSSD_ERR_SHAPE)
+ *   request_state_dev [n_requests]  out: 0, or 1 where lens[b] is negative, a parent is out of range, or a row does not follow all rows that lie 64 and more before it (up
+ *                 to 64 rows any tree will do, and so will one of up to 64 rows behind the end of a chain of any length).  All rows of such a request, and those that no
+ *                 request has, get position -1 and the word 0.
+ */
+knnssd_status knnssd_tree_tables(const int *lens_dev, const int *row_start_dev, const int *row_parent_dev, int n_requests, int n_rows,
+                                 int *row_pos_dev, unsigned long long *row_seen_dev, int *request_state_dev, void *cuda_stream);
+
+/*
+ * knnssd_paged_attention where row i of request b sees of the positions x = 0 .. lens[b] + i those with lens[b] + i - x >= 64 or that bit of row_seen[row] set.  A row
+ * whose word is 0 and that has no position 64 before it sees nothing: zeros.  Everything else as there.
+ */
+knnssd_status knnssd_tree_attention(const void *q_dev, int dtype, int n_rows, long long q_stride, int n_heads, int n_kv_heads,
+                                    int head_dim, const void *k_pages_dev, const void *v_pages_dev, int cache_dtype,
+                                    int page_size, int n_pages, const int *table_dev, int max_pages, const int *lens_dev,
+                                    const int *row_start_dev, const unsigned long long *row_seen_dev, int n_requests,
+                                    int max_fresh, float scale, void *out_dev, void *cuda_stream);
+
+/*
+ * Speculative sampling on trees, knnssd_spec_accept's rule with several drafts behind a row, for all requests at once.  p_dev [n_rows][vocab]: the full model's filtered
+ * distribution behind each row (it is taken to sum to 1); q_dev [n_rows][vocab]: the draft model's, where the drafts behind a row were drawn from its q, each by itself; NULL where
+ * they were chosen (by rank, say).  From row 0 on, the children of the row kept last are tested in row order.  With w what is left of its p, Z the sum of w (1 at first):
+ *   q given:  child c is kept iff u_accept[c] Z q(x_c) < w(x_c); else w becomes max(0, w / Z - q)
+ *   no q:     child c is kept iff u_accept[c] Z < w(x_c);        else w(x_c) becomes 0
+ * Behind the last row kept the token is the smallest x with w_0 + .. + w_x > u_final sum(w), drawn from p where nothing is left of it (-1 if p has no weight at all, or a
+ * NaN).  Tests and sums in 64 bits.  The tokens have p's distribution whatever was drafted.
+ *   row_token_dev [n_rows], row_parent_dev [n_rows]  in; a row whose token is outside [0, vocab), or whose parent is not a row before it, is passed over with all that follow it
+ *   u_accept_dev [n_rows], u_final_dev [n_requests]  uniforms in [0, 1) (u_final outside: token -1); those of rows 0 are not used
+ *   path_dev [n_rows]         out: path[row_start[b] + j] the j-th row kept, within its request, row 0 first; -1 behind the last one and for rows that no request has
+ *   n_accepted_dev, next_token_dev [n_requests]  out: drafts kept (rows behind row 0), the token after them; 0 and -1 for a request without rows
+ * Of a request the first KNNSSD_MAX_TREE_ROWS rows are looked at.  vocab at most KNNSSD_MAX_VOCAB, n_requests at most KNNSSD_MAX_REQUESTS: else KNNSSD_ERR_CAPACITY.
+ */
+#define KNNSSD_MAX_TREE_ROWS 1024
+#define KNNSSD_MAX_VOCAB (1 << 24)
+knnssd_status knnssd_tree_accept(const float *p_dev, const float *q_dev_or_null, int vocab, const int *row_token_dev,
+                                 const int *row_parent_dev, const int *row_start_dev, int n_requests, int n_rows,
+                                 const float *u_accept_dev, const float *u_final_dev, int *path_dev, int *n_accepted_dev,
+                                 int *next_token_dev, void *cuda_stream);
+
+/*
+ * The greedy form: a child is kept iff its token is row_best[its parent], the full model's choice behind that row; next_token = row_best[the last row kept].  Any number of
+ * rows, any tokens; the rest as in knnssd_tree_accept.
+ */
+knnssd_status knnssd_tree_agree(const int *row_best_dev, const int *row_token_dev, const int *row_parent_dev,
+                                const int *row_start_dev, int n_requests, int n_rows, int *path_dev, int *n_accepted_dev,
+                                int *next_token_dev, void *cuda_stream);
+
+/*
+ * K and V of the kept rows together: in each of n_pools pools (all layers' K and V) and for j = 0, 1, .. what lies at position lens[b] + path[row_start[b] + j] goes to
+ * lens[b] + j, as long as path ascends and stays below the request's rows.  Positions without a page are left out.
+ *   pools_host  HOST [n_pools] of DEVICE pointers, read during the call: pools of one type and size, as k_pages_dev above; cache_dtype, n_kv_heads, head_dim, page_size,
+ *               n_pages, max_pages and the limits on them as there
+ */
+knnssd_status knnssd_keep_rows(void *const *pools_host, int n_pools, int cache_dtype, int n_kv_heads, int head_dim, int page_size,
+                               int n_pages, const int *table_dev, int max_pages, const int *lens_dev, const int *row_start_dev,
+                               const int *path_dev, int n_requests, int n_rows, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,8 @@ EXPORTS = ["knnssd_init", "knnssd_destroy", "knnssd_prefill", "knnssd_select_ski
            "knnssd_gemm_split", "knnssd_linear_tc", "knnssd_build_anchors", "knnssd_cosine_top1", "knnssd_cosine_top1_static",
            "knnssd_debug_barrier_timeout", "knnssd_filtered_probs", "knnssd_sample_token", "knnssd_spec_accept",
            "knnssd_decode_sampled", "knnssd_page_tables", "knnssd_rotary_store", "knnssd_paged_attention", "knnssd_packed_attention",
-           "knnssd_attention_status", "knnssd_debug_attention_timeout"]
+           "knnssd_attention_status", "knnssd_debug_attention_timeout",
+           "knnssd_tree_tables", "knnssd_tree_attention", "knnssd_tree_accept", "knnssd_tree_agree", "knnssd_keep_rows"]
 
 
 class KnnssdError(RuntimeError):
@@ -95,6 +96,11 @@ def _load():
         "knnssd_paged_attention": (I, [P, I, I, L, I, I, I, P, P, I, I, I, P, I, P, P, I, I, F, P, P]),
         "knnssd_packed_attention": (I, [P, P, P, I, I, L, L, L, I, I, I, P, I, F, P, P]),
         "knnssd_attention_status": (I, [P]),
+        "knnssd_tree_tables": (I, [P, P, P, I, I, P, P, P, P]),
+        "knnssd_tree_attention": (I, [P, I, I, L, I, I, I, P, P, I, I, I, P, I, P, P, P, I, I, F, P, P]),
+        "knnssd_tree_accept": (I, [P, P, I, P, P, P, I, I, P, P, P, P, P, P]),
+        "knnssd_tree_agree": (I, [P, P, P, P, I, I, P, P, P, P]),
+        "knnssd_keep_rows": (I, [P, I, I, I, I, I, I, P, I, P, P, P, I, I, P]),
         "knnssd_debug_attention_timeout": (I, [C.c_uint, C.c_uint]),
     }
     for name, (res, args) in sigs.items():
@@ -278,6 +284,18 @@ def _i32(t: torch.Tensor, n: int, dev: int, what: str) -> int:
     return t.data_ptr()
 
 
+def _words(t: torch.Tensor, n: int, dev: int, what: str) -> int:
+    if t.dtype is not torch.int64 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int64 tensor of {n} values on the call's CUDA device")
+    return t.data_ptr()
+
+
+def _f32(t: torch.Tensor, n: int, dev: int, what: str) -> int:
+    if t.dtype is not torch.float32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 tensor of {n} values on the call's CUDA device")
+    return t.data_ptr()
+
+
 def _rows(t: torch.Tensor, dev: int, what: str) -> int:
     """Address of [rows][heads][head_dim] values whose heads are contiguous; the rows may be any distance apart."""
     if t.dim() != 3 or t.get_device() != dev or t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] > 1):
@@ -379,12 +397,7 @@ def _attention_out(q: torch.Tensor, dev: int, out: Optional[torch.Tensor]) -> to
     return out
 
 
-def knnssd_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
-                           row_start: torch.Tensor, max_fresh: int = 0, scale: Optional[float] = None,
-                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Attention of the new rows q [rows][n_heads][head_dim] over the requests' pages: row row_start[b] + i sees positions 0 .. lens[b] + i.
-    table [B][max_pages], lens [B], row_start [B + 1] int32.  max_fresh: the most rows of a request in this call, if known (a hint).  scale defaults to
-    head_dim ** -0.5."""
+def _over_pages(fn, name: str, q, k_pages, v_pages, table, lens, row_start, words, max_fresh, scale, out) -> torch.Tensor:
     dev = _device(q)
     n_pages, kv, page, hd = _pages(k_pages, v_pages, dev)
     dtype, cache = _type(q, "q"), _type(k_pages, "k_pages")
@@ -394,10 +407,20 @@ def knnssd_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
         raise ValueError("q's head_dim must be the pages', and table must be [requests][max_pages]")
     B, max_pages = table.shape
     out = _attention_out(q, dev, out)
-    _call(_lib.knnssd_paged_attention, "knnssd_paged_attention", dev, qp, dtype, rows, _row_stride(q), heads, kv, hd, k_pages.data_ptr(), v_pages.data_ptr(),
-          cache, page, n_pages, _i32(table, B * max_pages, dev, "table"), max_pages, _i32(lens, B, dev, "lens"), _i32(row_start, B + 1, dev, "row_start"), B, max_fresh,
+    seen = () if words is None else (_words(words, rows, dev, "row_seen"),)
+    _call(fn, name, dev, qp, dtype, rows, _row_stride(q), heads, kv, hd, k_pages.data_ptr(), v_pages.data_ptr(), cache, page, n_pages,
+          _i32(table, B * max_pages, dev, "table"), max_pages, _i32(lens, B, dev, "lens"), _i32(row_start, B + 1, dev, "row_start"), *seen, B, max_fresh,
           hd ** -0.5 if scale is None else scale, out.data_ptr())
     return out
+
+
+def knnssd_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                           row_start: torch.Tensor, max_fresh: int = 0, scale: Optional[float] = None,
+                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new rows q [rows][n_heads][head_dim] over the requests' pages: row row_start[b] + i sees positions 0 .. lens[b] + i.
+    table [B][max_pages], lens [B], row_start [B + 1] int32.  max_fresh: the most rows of a request in this call, if known (a hint).  scale defaults to
+    head_dim ** -0.5."""
+    return _over_pages(_lib.knnssd_paged_attention, "knnssd_paged_attention", q, k_pages, v_pages, table, lens, row_start, None, max_fresh, scale, out)
 
 
 def knnssd_packed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, scale: Optional[float] = None,
@@ -428,6 +451,78 @@ def knnssd_debug_attention_timeout(spin_limit: int, tiles: int = 0) -> None:
     rc = _lib.knnssd_debug_attention_timeout(spin_limit, tiles)
     if rc:
         raise KnnssdError(rc, "knnssd_debug_attention_timeout")
+
+
+# ---- drafts that branch ----
+def knnssd_tree_tables(lens: torch.Tensor, row_start: torch.Tensor, row_parent: torch.Tensor, row_pos: torch.Tensor, row_seen: torch.Tensor,
+                       request_state: torch.Tensor) -> None:
+    """Positions of the rows of the requests' trees and which of the rows before it each one sees, on the GPU.  lens [B], row_start [B + 1], row_parent [rows] int32 in;
+    row_pos [rows] int32, row_seen [rows] int64 (bit d: the position d before its own slot), request_state [B] int32 (0, or 1: no tree that the words can hold) out."""
+    dev = _device(lens)
+    B, rows = lens.numel(), row_parent.numel()
+    _call(_lib.knnssd_tree_tables, "knnssd_tree_tables", dev, _i32(lens, B, dev, "lens"), _i32(row_start, B + 1, dev, "row_start"), _i32(row_parent, rows, dev, "row_parent"),
+          B, rows, _i32(row_pos, rows, dev, "row_pos"), _words(row_seen, rows, dev, "row_seen"), _i32(request_state, B, dev, "request_state"))
+
+
+def knnssd_tree_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                          row_start: torch.Tensor, row_seen: torch.Tensor, max_fresh: int = 0, scale: Optional[float] = None,
+                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``knnssd_paged_attention`` where row row_start[b] + i sees of the positions 0 .. lens[b] + i those that lie 64 and more before its own and those d < 64
+    before it whose bit d of row_seen [rows] (int64, from ``knnssd_tree_tables``) is set."""
+    return _over_pages(_lib.knnssd_tree_attention, "knnssd_tree_attention", q, k_pages, v_pages, table, lens, row_start, row_seen, max_fresh, scale, out)
+
+
+def knnssd_tree_accept(p: torch.Tensor, q: Optional[torch.Tensor], row_token: torch.Tensor, row_parent: torch.Tensor, row_start: torch.Tensor,
+                       u_accept: torch.Tensor, u_final: torch.Tensor, path: torch.Tensor, n_accepted: torch.Tensor, next_token: torch.Tensor) -> None:
+    """Speculative sampling on the requests' trees, on the GPU.  p [rows][V] float32: the full model's filtered distribution behind each row; q [rows][V]: the draft
+    model's that the drafts behind a row were drawn from, None where they were chosen instead.  row_token, row_parent [rows], row_start [B + 1] int32 and the uniforms
+    u_accept [rows], u_final [B] in; path [rows] (row_start[b] + j: the j-th row kept, then -1), n_accepted [B], next_token [B] int32 out."""
+    dev = _device(p)
+    rows, B = row_token.numel(), u_final.numel()
+    if p.dim() != 2 or p.shape[0] != rows or (q is not None and q.shape != p.shape):
+        raise ValueError("p and q must be [rows][vocab]")
+    V = p.shape[1]
+    _call(_lib.knnssd_tree_accept, "knnssd_tree_accept", dev, _f32(p, rows * V, dev, "p"), None if q is None else _f32(q, rows * V, dev, "q"), V,
+          _i32(row_token, rows, dev, "row_token"), _i32(row_parent, rows, dev, "row_parent"), _i32(row_start, B + 1, dev, "row_start"), B, rows,
+          _f32(u_accept, rows, dev, "u_accept"), _f32(u_final, B, dev, "u_final"), _i32(path, rows, dev, "path"), _i32(n_accepted, B, dev, "n_accepted"),
+          _i32(next_token, B, dev, "next_token"))
+
+
+def knnssd_tree_agree(row_best: torch.Tensor, row_token: torch.Tensor, row_parent: torch.Tensor, row_start: torch.Tensor, path: torch.Tensor,
+                      n_accepted: torch.Tensor, next_token: torch.Tensor) -> None:
+    """The greedy form: a draft is kept if it is row_best [rows], the full model's choice, of the row before it.  All tensors int32."""
+    dev = _device(row_best)
+    rows, B = row_best.numel(), n_accepted.numel()
+    _call(_lib.knnssd_tree_agree, "knnssd_tree_agree", dev, _i32(row_best, rows, dev, "row_best"), _i32(row_token, rows, dev, "row_token"),
+          _i32(row_parent, rows, dev, "row_parent"), _i32(row_start, B + 1, dev, "row_start"), B, rows, _i32(path, rows, dev, "path"),
+          _i32(n_accepted, B, dev, "n_accepted"), _i32(next_token, B, dev, "next_token"))
+
+
+class PagePools:
+    """The K and V pools of all layers, for calls that go through all of them: tensors [n_pages][n_kv_heads][page_size][head_dim] of one type and device.  Keeps
+    references to them; make it once."""
+
+    def __init__(self, k_pages: Sequence[torch.Tensor], v_pages: Sequence[torch.Tensor]):
+        self._keep = (*k_pages, *v_pages)
+        if len(k_pages) != len(v_pages) or not self._keep:
+            raise ValueError("as many K pools as V pools, one at least")
+        self.device = _device(self._keep[0])
+        self.cache = _type(self._keep[0], "k_pages")
+        for t in self._keep:                                         # all as the first one
+            self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = _pages(self._keep[0], t, self.device)
+        self.pointers = (C.c_void_p * len(self._keep))(*[t.data_ptr() for t in self._keep])
+
+
+def knnssd_keep_rows(pools: PagePools, table: torch.Tensor, lens: torch.Tensor, row_start: torch.Tensor, path: torch.Tensor) -> None:
+    """K and V of the rows on the kept path, from the positions lens[b] + path[row_start[b] + j] to lens[b] + j in all pools.  table [B][max_pages], lens [B],
+    row_start [B + 1], path [rows] int32, path as ``knnssd_tree_accept`` leaves it."""
+    dev = pools.device
+    if table.dim() != 2:
+        raise ValueError("table must be [requests][max_pages]")
+    B, max_pages = table.shape
+    rows = path.numel()
+    _call(_lib.knnssd_keep_rows, "knnssd_keep_rows", dev, pools.pointers, len(pools.pointers), pools.cache, pools.n_kv_heads, pools.head_dim, pools.page_size, pools.n_pages,
+          _i32(table, B * max_pages, dev, "table"), max_pages, _i32(lens, B, dev, "lens"), _i32(row_start, B + 1, dev, "row_start"), _i32(path, rows, dev, "path"), B, rows)
 
 
 class Session:

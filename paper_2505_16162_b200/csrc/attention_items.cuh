@@ -37,7 +37,11 @@ struct Args {
     // bounded waits (tensor kernel): where one that gives up leaves its code, after how many polls; tiles that a block's copies end after
     int *err;
     unsigned wait_limit, stop_after;
+    const unsigned long long *seen;       // trees: [R], which of the 64 positions up to a row's own it sees
 };
+
+// Which positions a row of a tree sees: all that lie 64 and more before its own, and of those d = 0 .. 63 before it the ones whose bit d is set.
+__device__ __forceinline__ bool tree_sees(unsigned long long word, int d) { return d >= 64 || (d >= 0 && (word >> d & 1)); }
 
 // first: no run before this one begins within the item; [from, to): the run's positions of it; start: the item (-1: none)
 struct Part { long long start; int first, kv, from, to, row0, rows, vh, paired; };
@@ -226,23 +230,24 @@ template <int N> __device__ __forceinline__ void read_values(const bf16_t *p, fl
     for (int i = 0; i < N; i += 2) { v[i] = __uint_as_float(w[i / 2] << 16); v[i + 1] = __uint_as_float(w[i / 2] & 0xffff0000u); }
 }
 
-// A row of an item: its place among all rows and its head, the positions from .. to - 1 that it is about, and where its result goes.
-struct Row { int b, seq_row0, row, head, from, to; bool whole; size_t slot; };
+// A row of an item: its place among all rows and its head, the positions from .. to - 1 that it is about, where its result goes, and its own position.
+struct Row { int b, seq_row0, row, head, from, to; bool whole; size_t slot; int last; };
 
 // The same row from nothing but the positions that it sees, in ordinary fp32 arithmetic: whatever IEEE makes of values that are not finite.  A warp
 // together, a score a lane, then HD / 32 dimensions a lane.  For rows that the matrix instructions cannot do; never on finite inputs.
-template <int HD, typename QT, typename KT, bool PAGED> __device__ __noinline__ void row_by_definition(const Args &a, const Row r) {
+template <int HD, typename QT, typename KT, bool PAGED, bool TREE> __device__ __noinline__ void row_by_definition(const Args &a, const Row r) {
     constexpr int D = HD / 32, N = 16 / (int)sizeof(KT);             // dimensions a lane; values of 16 bytes of a key
     const int lane = threadIdx.x & 31, kvh = r.head / (a.H / a.KV);
     const QT *q = static_cast<const QT *>(a.q) + (size_t)r.row * a.q_stride + (size_t)r.head * HD;
     const KT *kp = static_cast<const KT *>(a.k), *vp = static_cast<const KT *>(a.v) + lane * D;
+    const unsigned long long word = TREE ? a.seen[r.row] : 0ull;
     float o[D], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int j = 0; j < D; ++j) o[j] = 0.f;
 #pragma unroll 1
     for (int p0 = r.from; p0 < r.to; p0 += 32) {
         size_t k = 0, v = 0;
-        const bool there = p0 + lane < r.to && key_at<HD, PAGED>(a, r.b, r.seq_row0, kvh, p0 + lane, k, v);
+        const bool there = p0 + lane < r.to && (!TREE || tree_sees(word, r.last - p0 - lane)) && key_at<HD, PAGED>(a, r.b, r.seq_row0, kvh, p0 + lane, k, v);
         float s = -INFINITY;
         if (there) {
             s = 0.f;

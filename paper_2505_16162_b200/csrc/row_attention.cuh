@@ -66,7 +66,7 @@ template <int HD, typename KT> struct Ring {
     __device__ static __forceinline__ int vswz(int p, int c) { return sizeof(KT) == 2 ? c ^ (p & 7) : c ^ (((p >> 1) & 3) << 1); }
 };
 
-template <int HD, typename KT, bool PAGED>
+template <int HD, typename KT, bool PAGED, bool TREE = false>
 __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const __grid_constant__ Args a) {
     using Rg = Ring<HD, KT>;
     constexpr int NT = Rg::WARPS * 32, NQ = 3, NK = sizeof(KT) == 4 ? 3 : 1, KS = HD / 16, NTILE = HD / 8;
@@ -179,11 +179,13 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
             auto dim_of = [&](int s, int h) { return sizeof(KT) == 2 ? 32 * (s >> 1) + 8 * t + 4 * (s & 1) + 2 * h : 16 * s + 4 * t + 2 * h; };
             uint32_t qf[KS][NQ][4];
             int last[2];                                             // the last position a row sees; -1: no such row
+            unsigned long long word[2];                              // trees: which of the 64 up to it
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int r = 8 * e + g, tok = r / heads;
                 const bool on = r < live;
                 last[e] = on ? seen0 + tok : -1;
+                word[e] = TREE && on ? __ldg(a.seen + row0 + tok) : 0ull;
                 const float *qp = static_cast<const float *>(a.q) + (long long)(row0 + tok) * a.q_stride + (long long)(h0 + r % heads) * HD;
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                         }
                     }
                 }
-                const bool ragged = hole || p + TP - 1 > seen0;      // some row does not see all of these positions
+                const bool ragged = hole || p + TP - 1 > seen0 - (TREE ? 64 : 0);      // some row may not see all of these positions
                 uint32_t pf[NQ][4];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -256,7 +258,7 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                     if (ragged) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (hole || p + 8 * (i >> 1) + 2 * t + (i & 1) > last[e]) x[i] = -INFINITY;
+                            if (hole || (TREE ? !tree_sees(word[e], last[e] - p - 8 * (i >> 1) - 2 * t - (i & 1)) : p + 8 * (i >> 1) + 2 * t + (i & 1) > last[e])) x[i] = -INFINITY;
                     }
                     float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -364,7 +366,8 @@ __global__ void __launch_bounds__(Ring<HD, KT>::WARPS * 32, 1) rows_kernel(const
                 __syncwarp();                                        // behind the other lanes' stores
                 for (int r = 0; r < live; ++r)
                     if (odd[r >> 3] >> (4 * (r & 7)) & 15u)
-                        row_by_definition<HD, float, KT, PAGED>(a, Row{it.b, it.r.row0, row0 + r / heads, h0 + r % heads, from, min(seen0 + r / heads + 1, to), whole, slot + r});
+                        row_by_definition<HD, float, KT, PAGED, TREE>(
+                            a, Row{it.b, it.r.row0, row0 + r / heads, h0 + r % heads, from, min(seen0 + r / heads + 1, to), whole, slot + r, seen0 + r / heads});
             }
         }
         any = it.next(a) && it.start < x1;

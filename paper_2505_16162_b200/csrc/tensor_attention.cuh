@@ -282,7 +282,7 @@ struct Mine {
 // finite): the same by the definition, a row a warp.  Positions behind an item's last are zero in the tiles, so only the item's own new positions can
 // do it.  Never on finite inputs.  It comes behind the block's last item, when no wait is left that could run out meanwhile: 12000 packed tokens with such a V
 // every 64 rows take 170 ms for 0.79, two requests of 120 thousand positions with one each 8.0 for 0.24.
-template <int HD, bool PAGED> __device__ __noinline__ void mend_rows(const Args &a, const Costs<NCOST> &costs, int w, long long x0, long long x1) {
+template <int HD, bool PAGED, bool TREE> __device__ __noinline__ void mend_rows(const Args &a, const Costs<NCOST> &costs, int w, long long x0, long long x1) {
     constexpr int PIECES = HD / 8;                                   // 16-byte pieces of a position
     const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31;
     Item<true> it = item_at<true>(a, costs, x0);
@@ -297,9 +297,11 @@ template <int HD, bool PAGED> __device__ __noinline__ void mend_rows(const Args 
             bool odd = false, disturbed = false;
             for (int i = lane; i < HD; i += 32) odd |= !isfinite(mine.whole ? bf16_bits_to_float(out[i]) : a.o[slot * HD + i]);
             if (!__any_sync(0xffffffffu, odd)) continue;
-            const int end = min(min(job.to, job.from + mine.steps * SUB), it.kv), hidden = max(mine.last + 1, job.from);
+            const int end = min(min(job.to, job.from + mine.steps * SUB), it.kv), hidden = max(mine.last + (TREE ? -63 : 1), job.from);
+            const unsigned long long word = TREE ? a.seen[mine.row] : 0ull;
             for (int i = lane; i < (end - hidden) * PIECES; i += 32) {
                 size_t k, v;
+                if (TREE && tree_sees(word, mine.last - hidden - i / PIECES)) continue;
                 if (!key_at<HD, PAGED>(a, it.b, it.r.row0, mine.head / (a.H / a.KV), hidden + i / PIECES, k, v)) continue;
                 float y[8];
                 read_values(static_cast<const bf16_t *>(a.v) + v + i % PIECES * 8, y);
@@ -307,7 +309,7 @@ template <int HD, bool PAGED> __device__ __noinline__ void mend_rows(const Args 
                 for (int j = 0; j < 8; ++j) disturbed |= !isfinite(y[j]);
             }
             if (__any_sync(0xffffffffu, disturbed))
-                row_by_definition<HD, bf16_t, bf16_t, PAGED>(a, Row{it.b, it.r.row0, mine.row, mine.head, job.from, min(mine.last + 1, end), mine.whole, slot});
+                row_by_definition<HD, bf16_t, bf16_t, PAGED, TREE>(a, Row{it.b, it.r.row0, mine.row, mine.head, job.from, min(mine.last + 1, end), mine.whole, slot, mine.last});
         }
     } while (it.next(a) && it.start < x1);
 }
@@ -332,7 +334,7 @@ template <int HD> __device__ __noinline__ void spoil_rows(const Args &a, const C
     } while (it.next(a) && it.start < x1);
 }
 
-template <int HD, int MODE>
+template <int HD, int MODE, bool TREE = false>
 __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                                                         const __grid_constant__ CUtensorMap vmap) {
     using L = Lay<HD>;
@@ -621,6 +623,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 const int token = mine.token, last = mine.last, row = mine.row * a.H + mine.head, steps = mine.steps;
                 const int first_last = job.seen0 + (job.paired ? 0 : h * a.tb);
                 const bool live = __any_sync(0xffffffffu, token >= 0);
+                const unsigned long long word = TREE && token >= 0 ? __brevll(__ldg(a.seen + mine.row)) : 0ull;      // bit 63 - d: the position d before the row's own
                 float m = -INFINITY, l = 0.f;
                 for (int u = 0; u < steps && ok; ++u, ++done) {
                     const uint32_t bar = 8 * (2 * h + (done & 1)), s_at = lanes + h * KEYS + (done & 1) * SUB;
@@ -640,11 +643,15 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                     settle(x[0]);
                     settle(x[1]);
                     const unsigned groups = PAGED ? info[(step0 + (u >> 1)) % INFO] >> (4 * (u & 1)) & 15u : 15u;
-                    if (k0 + SUB - 1 > first_last || groups != 15u) {            // what a row does not see is made -inf
+                    if (k0 + SUB - 1 > first_last - (TREE ? 64 : 0) || groups != 15u) {            // what a row does not see is made -inf
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const int n = last - k0 - 32 * c;        // the row sees keys 0 .. n of the 32
                             uint32_t seen = n >= 31 ? 0xffffffffu : n < 0 ? 0u : (2u << n) - 1;
+                            if (TREE && n < 64 + 31) {               // some of the 32 are less than 64 positions before the row's own, or behind it
+                                const int s = 63 - n;                // the word's bit of the first one
+                                seen = s >= 64 ? 0u : s >= 0 ? (uint32_t)(word >> s) : (uint32_t)(word << -s) | ((1u << -s) - 1);
+                            }
                             if (PAGED) seen &= ((groups >> (2 * c) & 1) ? 0xffffu : 0u) | ((groups >> (2 * c) & 2) ? 0xffff0000u : 0u);
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
@@ -784,7 +791,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
     }
     if (quit) spoil_rows<HD>(a, costs, w, x0, x1);
-    else if (odd) mend_rows<HD, PAGED>(a, costs, w, x0, x1);
+    else if (odd) mend_rows<HD, PAGED, TREE>(a, costs, w, x0, x1);
 }
 
 }  // namespace tcattn
