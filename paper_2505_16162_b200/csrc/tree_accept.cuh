@@ -9,7 +9,7 @@
 //
 // A request is the work of a cluster of C blocks, each with a contiguous part of the ids.  All blocks take the same decisions from the same numbers: the tests need one value
 // of p and of q a draft, fetched for all drafts at once at the start.  Only a rejection reads a row: a pass over the ids, a sum per warp, a meeting of the cluster.  The last pass's sums
-// are the draw's: the block and the warp whose ids hold the crossing are known from them, the block walks that warp's ids.  Without q a node takes one pass whatever is
+// are the draw's: the block and the warp whose ids hold the crossing are known from them, that block goes on in that warp's ids.  Without q a node takes one pass whatever is
 // rejected: the sum of all ids but its children's, to which the children not yet rejected are added (nothing is subtracted, so nothing cancels).
 // Sums in 64 bits: what a test or a draw next to a border decides does not depend on the order of 150 thousand additions.
 #pragma once
@@ -24,9 +24,17 @@ namespace trees {
 
 namespace cg = cooperative_groups;
 
-constexpr int ACC_NT = 512, ACC_NW = ACC_NT / 32;
+constexpr int ACC_NT = 256, ACC_NW = ACC_NT / 32;
 constexpr int ACC_ROWS = 1024;            // rows of a request that are looked at
-constexpr int ACC_AHEAD = 8;              // values of a row that a thread has on their way
+// Blocks of a request: as many as find room at once, and a thousand ids at least for each, below that a meeting of more blocks costs what they save.  1 / 2 / 4 / 8 / 16 of
+// them, drafts drawn: 24 requests of 25 rows and 1000 ids 7.6 / 10 / 10 / 10 / 16 us, of 32000 24 / 17 / 13 / 12 / 13, of 152064 86 / 49 / 31 / 22 / 17; 400 requests of 9 rows and
+// 32000 ids 41 / 39 / 47 / 68 / 127.  With more than 4096 ids a block they pay up to three and a half a processor (32 requests of 152064 ids as 16 blocks 21 us, as 8 28), else
+// up to two.
+inline int blocks_of(int requests, int vocab, int processors) {
+    for (int c = 16; c > 1; c /= 2)
+        if (2ll * requests * c <= (vocab > 4096 * c ? 7 : 4) * processors && vocab >= 1000 * c) return c;
+    return 1;
+}
 
 struct AcceptArgs {
     const float *p, *q;                   // [R][V]; q null: drafts chosen
@@ -37,8 +45,9 @@ struct AcceptArgs {
     int *path, *accepted, *next;
 };
 
-struct AcceptShared {
-    double warp_sum[ACC_NW], slot[2][16], inv[ACC_ROWS];             // inv: 1 / Z of the rejections at the node
+template <int C> struct AcceptShared {
+    double slot[2][C * ACC_NW];                                      // the sums of all blocks' warps; the next pass's may come while these are read
+    double part[ACC_NW];
     float p_of[ACC_ROWS], q_of[ACC_ROWS], u[ACC_ROWS];               // of each row: its parent's p and q at its token, its uniform
     int parent[ACC_ROWS], token[ACC_ROWS];                           // parent -1: not to be tested
 };
@@ -48,137 +57,247 @@ __device__ __forceinline__ double warp_sum64(double v) {
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+__device__ __forceinline__ double warp_upto64(double v) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double t = __shfl_up_sync(0xffffffffu, v, o);
+        if ((threadIdx.x & 31) >= o) v += t;
+    }
+    return v;
+}
 
 // The lowest row behind `last` whose parent is `node`; n: there is none.  The same in every warp.
-__device__ __forceinline__ int next_child(const AcceptShared &sh, int n, int node, int last) {
+__device__ __forceinline__ int next_child(const int *parent, int n, int node, int last) {
     for (int i0 = (last + 1) & ~31; i0 < n; i0 += 32) {
         const int i = i0 + (threadIdx.x & 31);
-        const unsigned found = __ballot_sync(0xffffffffu, i > last && i < n && sh.parent[i] == node);
+        const unsigned found = __ballot_sync(0xffffffffu, i > last && i < n && parent[i] == node);
         if (found) return i0 + __ffs(found) - 1;
     }
     return n;
 }
 
-// What a row's weights are: its values; what is left after `m` rejections of drafts drawn from q; its values without those of the children of `node`.
+// What a row's weights are: its values; what rejections of drafts drawn from q have left, which is max(0, a p - b q) whatever their number (max(0, y) / Z - q and
+// y / Z - q have the same positive part); its values without those of the children of `node`.
 enum { ALL = 0, DRAWN = 1, CHOSEN = 2 };
-struct Weights { const float *p, *q; int kind, m, node, n; };
+struct Weights { const float *p, *q; int kind, node, n; double a, b; };
+__device__ __forceinline__ double left_of(double a, double b, float p, float q) { return fmax(fma(a, (double)p, -b * (double)q), 0.0); }
+template <int C> __device__ __forceinline__ int child_token(const AcceptShared<C> &sh, const Weights &w, int i) { return i < w.n && sh.parent[i] == w.node ? sh.token[i] : -1; }
 
-// The ids among 32 from `base` on that are tokens of the node's children, as bits.  t0, t1: this lane's of the first 64 rows, -1 where it is no child's.
-__device__ __forceinline__ unsigned childrens_ids(const AcceptShared &sh, const Weights &w, int t0, int t1, int base) {
-    unsigned mine = 0;
-    if (t0 >= base && t0 < base + 32) mine |= 1u << (t0 - base);
-    if (t1 >= base && t1 < base + 32) mine |= 1u << (t1 - base);
-    for (int i = 64 + (threadIdx.x & 31); i < w.n; i += 32)
-        if (sh.parent[i] == w.node && sh.token[i] >= base && sh.token[i] < base + 32) mine |= 1u << (sh.token[i] - base);
-    return __reduce_or_sync(0xffffffffu, mine);
-}
-__device__ __forceinline__ int child_token(const AcceptShared &sh, const Weights &w, int i) { return w.kind == CHOSEN && i < w.n && sh.parent[i] == w.node ? sh.token[i] : -1; }
-__device__ __forceinline__ double weight_of(const AcceptShared &sh, const Weights &w, float p, float q) {
-    double x = p;
-    if (w.kind == DRAWN)
-        for (int k = 0; k < w.m; ++k) x = fmax(fma(x, sh.inv[k], -(double)q), 0.0);
-    return x;
-}
-
-// Ids of a warp's part of a range of `len`.
-__device__ __forceinline__ int part_of(int len) { return ((len + ACC_NW - 1) / ACC_NW + 31) & ~31; }
-
-// The sum of the weights of ids [lo, hi), a part per warp: sh.warp_sum.  Behind it the block has met.
-__device__ __forceinline__ void sum_part(AcceptShared &sh, const Weights &w, int lo, int hi) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = part_of(hi - lo);
-    const int i0 = (int)min((long long)hi, lo + (long long)warp * part), i1 = min(hi, i0 + part);
-    const int t0 = child_token(sh, w, lane), t1 = child_token(sh, w, lane + 32);
-    bool here = (t0 >= i0 && t0 < i1) || (t1 >= i0 && t1 < i1);
-    for (int i = 64 + lane; i < w.n; i += 32) { const int t = child_token(sh, w, i); here |= t >= i0 && t < i1; }
-    const bool some = __any_sync(0xffffffffu, here);                 // a child's token is among the warp's ids
+// A lane's share of a sum over ids [i0, i1), N values of a row on their way.  Pieces of code of their own: a round calls them from several places, and a block that comes to an
+// instruction for the first time waits for it (unrolled in place, 32 values at a time and the draw's running sums with them: one row of 152064 ids 19 us for 7).
+// A float's bits, moved to where a double has its own, are its value times 2^-896, zeros and subnormals included; the sum is scaled back.  Two integer operations, where a
+// conversion takes 11 clocks a warp (a row of 152064 ids by one block: 32 us so, 24 with the bits).  What is not a finite number, or has a sign, is done by conversions.
+constexpr int OUTS = 4;                   // ids that a sum of values can leave out
+constexpr double SCALED_BACK = 0x1p896;
+__device__ __forceinline__ double scaled(unsigned bits) { return __hiloint2double(bits >> 3, bits << 29); }
+static __device__ __noinline__ double sum_values(const float *p, int i0, int i1, int out0, int out1, int out2, int out3) {
+    constexpr int N = 8;
     double s[2] = {0.0, 0.0};
-    for (int base = i0; base < i1; base += 32 * ACC_AHEAD) {
-        float p[ACC_AHEAD], q[ACC_AHEAD];
+    unsigned top = 0;
+    auto in = [&](int id) { return id < i1 && id != out0 && id != out1 && id != out2 && id != out3; };
+    i0 += threadIdx.x & 31;
+#pragma unroll 1
+    for (int i = i0; i < i1; i += 32 * N) {
+        unsigned v[N];
 #pragma unroll
-        for (int e = 0; e < ACC_AHEAD; ++e) {
-            const int i = base + 32 * e + lane;
-            p[e] = i < i1 ? w.p[i] : 0.f;
-            q[e] = w.kind == DRAWN && i < i1 ? w.q[i] : 0.f;
+        for (int e = 0; e < N; ++e) v[e] = in(i + 32 * e) ? __float_as_uint(p[i + 32 * e]) : 0u;
+#pragma unroll
+        for (int e = 0; e < N; ++e) { s[e & 1] += scaled(v[e]); top = max(top, v[e]); }
+    }
+    if (top < 0x7f800000u) return (s[0] + s[1]) * SCALED_BACK;
+    double t = 0.0;
+#pragma unroll 1
+    for (int i = i0; i < i1; i += 32) t += in(i) ? (double)p[i] : 0.0;
+    return t;
+}
+static __device__ __noinline__ double sum_left(const float *p, const float *q, double a, double b, int i0, int i1) {
+    constexpr int N = 8;
+    double s[2] = {0.0, 0.0};
+    unsigned top = 0;
+    i0 += threadIdx.x & 31;
+#pragma unroll 1
+    for (int i = i0; i < i1; i += 32 * N) {
+        unsigned v[N], u[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            v[e] = i + 32 * e < i1 ? __float_as_uint(p[i + 32 * e]) : 0u;
+            u[e] = i + 32 * e < i1 ? __float_as_uint(q[i + 32 * e]) : 0u;
         }
 #pragma unroll
-        for (int e = 0; e < ACC_AHEAD; ++e) {
-            const double x = weight_of(sh, w, p[e], q[e]);
-            const bool out = some && (childrens_ids(sh, w, t0, t1, base + 32 * e) >> lane & 1);
-            s[e & 1] += out ? 0.0 : x;
+        for (int e = 0; e < N; ++e) {
+            const double x = fma(a, scaled(v[e]), -b * scaled(u[e]));
+            s[e & 1] += __double2hiint(x) < 0 ? 0.0 : x;
+            top = max(top, max(v[e], u[e]));
         }
     }
-    const double all = warp_sum64(s[0] + s[1]);
-    __syncthreads();                                                 // the sums before have been read
-    if (lane == 0) sh.warp_sum[warp] = all;
-    __syncthreads();
+    if (top < 0x7f800000u) return (s[0] + s[1]) * SCALED_BACK;
+    double t = 0.0;
+#pragma unroll 1
+    for (int i = i0; i < i1; i += 32) t += left_of(a, b, p[i], q[i]);
+    return t;
+}
+// Whether an id is the token of a child, for the 32 ids from `base` on.
+template <int C> __device__ __forceinline__ bool childs_id(const AcceptShared<C> &sh, const Weights &w, int base) {
+    unsigned out = 0;
+    for (int i = threadIdx.x & 31; i < w.n; i += 32) {
+        const int t = child_token(sh, w, i);
+        if (t >= base && t < base + 32) out |= 1u << (t - base);
+    }
+    return __reduce_or_sync(0xffffffffu, out) >> (threadIdx.x & 31) & 1;
+}
+// The lowest token of a child above `id`; INT_MAX: none is.
+template <int C> __device__ __forceinline__ int next_token(const AcceptShared<C> &sh, const Weights &w, int id) {
+    int t = INT_MAX;
+    for (int i = threadIdx.x & 31; i < w.n; i += 32) {
+        const int x = child_token(sh, w, i);
+        if (x > id) t = min(t, x);
+    }
+    return __reduce_min_sync(0xffffffffu, t);
+}
+// The sum of the weights of ids [i0, i1), by a warp.
+template <int C> __device__ __forceinline__ double sum_of(const AcceptShared<C> &sh, const Weights &w, int i0, int i1) {
+    const int lane = threadIdx.x & 31;
+    double s = 0.0;
+    if (w.kind == DRAWN) s = sum_left(w.p, w.q, w.a, w.b, i0, i1);
+    else {
+        for (int from = i0, to; from < i1; from = to) {              // runs of ids with OUTS of the children's tokens among them, or all
+            int out[OUTS];
+#pragma unroll
+            for (int k = 0, t = from - 1; k < OUTS; ++k) out[k] = t = w.kind == CHOSEN && t < i1 ? next_token(sh, w, t) : INT_MAX;
+            to = out[OUTS - 1] < i1 ? min(i1, next_token(sh, w, out[OUTS - 1])) : i1;
+            s += sum_values(w.p, from, to, out[0], out[1], out[2], out[3]);
+        }
+    }
+    return warp_sum64(s);
 }
 
-// The same over all ids, for all blocks of the cluster: their sums are in sh.slot[turn].
-template <int C> __device__ __forceinline__ double sum_all(AcceptShared &sh, const Weights &w, int lo, int hi, int turn) {
-    cg::cluster_group cluster = cg::this_cluster();
-    sum_part(sh, w, lo, hi);
-    if (threadIdx.x < C) {
-        double mine = 0.0;
-#pragma unroll
-        for (int k = 0; k < ACC_NW; ++k) mine += sh.warp_sum[k];
-        cluster.map_shared_rank(&sh, threadIdx.x)->slot[turn][cluster.block_rank()] = mine;
+// Ids of a warp's part of a range of `len`, and where warp k's begins.
+__device__ __forceinline__ int part_of(int len) { return ((len + ACC_NW - 1) / ACC_NW + 31) & ~31; }
+__device__ __forceinline__ int part_at(int lo, int hi, int k) { return (int)min((long long)hi, lo + (long long)k * part_of(hi - lo)); }
+
+// The sum of the weights over all ids, [lo, hi) this block's: a part a warp, whose sum goes to all blocks; then the cluster meets.
+template <int C> __device__ __forceinline__ double sum_all(AcceptShared<C> &sh, const Weights &w, int lo, int hi, int turn) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const double mine = sum_of(sh, w, part_at(lo, hi, warp), part_at(lo, hi, warp + 1));
+    if constexpr (C > 1) {
+        cg::cluster_group cluster = cg::this_cluster();
+        if (lane < C) cluster.map_shared_rank(&sh, lane)->slot[turn][cluster.block_rank() * ACC_NW + warp] = mine;
+        cluster.sync();
+    } else {
+        if (lane == 0) sh.slot[turn][warp] = mine;
+        __syncthreads();
     }
-    cluster.sync();
-    double total = 0.0;
+    double s = 0.0;
 #pragma unroll
-    for (int r = 0; r < C; ++r) total += sh.slot[turn][r];
-    return total;
+    for (int i = 0; i < (C * ACC_NW + 31) / 32; ++i)
+        if (C * ACC_NW >= 32 || lane < C * ACC_NW) s += sh.slot[turn][lane * ((C * ACC_NW + 31) / 32) + i];
+    return __shfl_sync(0xffffffffu, warp_upto64(s), 31);
 }
 
-// By the block whose ids hold the crossing, behind a sum over its ids [lo, hi): the first id at which the running sum, `before` ahead of them, passes `target`.
-__device__ __forceinline__ int find_id(AcceptShared &sh, const Weights &w, int lo, int hi, double before, double target) {
-    for (;;) {
-        int k = 0;
-        double e = before;
-        while (k < ACC_NW && !(e + sh.warp_sum[k] > target)) e += sh.warp_sum[k++];
-        if (k == ACC_NW) {                                           // rounding hides it: the last id with weight
-            target = INFINITY;
-            while (k > 0 && !(sh.warp_sum[--k] > 0.0)) {}
-        }
-        before = e;
-        const int part = part_of(hi - lo);
-        lo = min(hi, lo + k * part);
-        hi = min(hi, lo + part);
-        if (hi - lo <= 128) break;
-        sum_part(sh, w, lo, hi);
-    }
-    int token = -1;
-    if (threadIdx.x < 32) {
-        const int lane = threadIdx.x, t0 = child_token(sh, w, lane), t1 = child_token(sh, w, lane + 32);
-        for (int base = lo; base < hi; base += 32) {
-            const int i = base + lane;
-            double x = i < hi ? weight_of(sh, w, w.p[i], w.kind == DRAWN ? w.q[i] : 0.f) : 0.0;
-            if (w.kind == CHOSEN && (childrens_ids(sh, w, t0, t1, base) >> lane & 1)) x = 0.0;
-            double upto = x;
+// Of N sums one behind the other, `before` ahead of them, the one in which the running sum passes `target`, and what is ahead of it.  The lanes' running sums are rounded
+// otherwise than a lane's own: where the crossing lies between the two it is in the last sum up to there that is not zero, at its end (the target becomes infinite).  By a warp.
+template <int N> __device__ __forceinline__ int crossing(const double *sums, double &before, double &target) {
+    constexpr int PER = (N + 31) / 32;
+    const int lane = threadIdx.x & 31;
+    double own = 0.0;
+    int last = -1;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double t = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += t;
+    for (int i = 0; i < PER; ++i)
+        if (lane * PER + i < N) {
+            const double v = sums[lane * PER + i];
+            own += v;
+            if (v > 0.0) last = lane * PER + i;
+        }
+    const double upto = before + warp_upto64(own);
+    const unsigned past = __ballot_sync(0xffffffffu, upto > target);
+    double e = __shfl_up_sync(0xffffffffu, upto, 1);
+    if (lane == 0) e = before;
+    int at = -1;
+    if (past && lane == __ffs(past) - 1) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (at < 0 && lane * PER + i < N) {
+                const double v = sums[lane * PER + i];
+                if (e + v > target) at = lane * PER + i; else e += v;
             }
-            const unsigned past = __ballot_sync(0xffffffffu, x > 0.0 && before + upto > target), some = __ballot_sync(0xffffffffu, x > 0.0);
-            if (past) { token = base + __ffs(past) - 1; break; }
-            if (some) token = base + 31 - __clz(some);
-            before += __shfl_sync(0xffffffffu, upto, 31);
-        }
     }
-    return token;
+    if (past) {
+        at = __shfl_sync(0xffffffffu, at, __ffs(past) - 1);
+        before = __shfl_sync(0xffffffffu, e, __ffs(past) - 1);
+        if (at >= 0) return at;
+        if (lane >= __ffs(past)) last = -1;
+    }
+    target = INFINITY;
+    return max(0, __reduce_max_sync(0xffffffffu, last));
 }
 
-template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC_NT) tree_accept_kernel(const AcceptArgs a) {
+// By a block: the first of the ids [lo, hi) at which the running sum, `before` ahead of them, passes `target`; in one of its warps, the others get -1.
+template <int C> __device__ __forceinline__ int find_id(AcceptShared<C> &sh, const Weights &w, int lo, int hi, double before, double target) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    while (hi - lo > ACC_NT) {
+        const double mine = sum_of(sh, w, part_at(lo, hi, warp), part_at(lo, hi, warp + 1));
+        __syncthreads();                                             // the sums before have been read
+        if (lane == 0) sh.part[warp] = mine;
+        __syncthreads();
+        const int k = crossing<ACC_NW>(sh.part, before, target), at = part_at(lo, hi, k);
+        hi = part_at(lo, hi, k + 1);
+        lo = at;
+    }
+    const int base = lo + 32 * warp, id = base + lane;               // an id a thread
+    double x = 0.0;
+    if (id < hi) x = w.kind == DRAWN ? left_of(w.a, w.b, w.p[id], w.q[id]) : (double)w.p[id];
+    if (w.kind == CHOSEN && childs_id(sh, w, base)) x = 0.0;
+    const double upto = warp_upto64(x);
+    __syncthreads();
+    if (lane == 31) sh.part[warp] = upto;
+    __syncthreads();
+    if (warp != crossing<ACC_NW>(sh.part, before, target)) return -1;
+    const unsigned past = __ballot_sync(0xffffffffu, x > 0.0 && before + upto > target), some = __ballot_sync(0xffffffffu, x > 0.0);
+    return past ? base + __ffs(past) - 1 : some ? base + 31 - __clz(some) : base;
+}
+
+// Drafts chosen: of the children of w.node behind row c, which was rejected, the first that is kept; `rest`: the sum without all of the node's children.  n: none is.
+// The sum that a child is held against is the rest and the children from it on: all are tested at once.  The same in every warp.
+template <int C> __device__ __forceinline__ int first_kept(const AcceptShared<C> &sh, const Weights &w, int c, double rest) {
+    const int lane = threadIdx.x & 31;
+    auto p_of = [&](int i) { return i > c && i < w.n && sh.parent[i] == w.node ? (double)sh.p_of[i] : 0.0; };
+    auto from_here_on = [&](double v) {                              // the sum over this lane and those behind it
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double t = __shfl_down_sync(0xffffffffu, v, o);
+            if (lane + o < 32) v += t;
+        }
+        return v;
+    };
+    static_assert(ACC_ROWS <= 32 * 32, "a lane for 32 rows");
+    double later = 0.0;                                              // lane k: children among the rows from 32 (k + 1) on
+    if (w.n > 32) {
+        for (int k = 1; 32 * k < w.n; ++k) {
+            const double s = warp_sum64(p_of(32 * k + lane));
+            if (lane == k - 1) later = s;
+        }
+        later = from_here_on(later);
+    }
+    for (int k = (c + 1) / 32; 32 * k < w.n; ++k) {
+        const int i = 32 * k + lane;
+        const double mine = p_of(i), sum = rest + __shfl_sync(0xffffffffu, later, k) + from_here_on(mine);
+        const unsigned found = __ballot_sync(0xffffffffu, i > c && i < w.n && sh.parent[i] == w.node && (double)sh.u[i] * sum < mine);
+        if (found) return 32 * k + __ffs(found) - 1;
+    }
+    return w.n;
+}
+
+template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC_NT, 3) tree_accept_kernel(const AcceptArgs a) {
     chain_wait();
-    __shared__ AcceptShared sh;
+    __shared__ AcceptShared<C> sh;
     cg::cluster_group cluster = cg::this_cluster();
-    cluster.barrier_arrive();                                        // every block has to run before another writes to its shared memory
-    const int b = blockIdx.x / C, rank = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, V = a.V;
+    if (C > 1) cluster.barrier_arrive();                             // every block has to run before another writes to its shared memory
+    const int b = blockIdx.x / C, rank = C > 1 ? (int)cluster.block_rank() : 0, tid = threadIdx.x, lane = tid & 31, V = a.V;
     each_other_row(a.row_start, a.B, a.R, [&](int r) { a.path[r] = -1; });
     int row0, n_all;
     rows_of(a.row_start, a.R, b, row0, n_all);
     const int n = min(n_all, ACC_ROWS);
+    const float u_final = a.u_final[b];
     for (int i = tid; i < n; i += ACC_NT) {
         const int up = a.parent[row0 + i], x = a.token[row0 + i];
         const bool tested = i > 0 && up >= 0 && up < i && x >= 0 && x < V;
@@ -199,65 +318,59 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
         }
         __syncthreads();
     }
-    const float u_final = a.u_final[b];
-    cluster.barrier_wait();
-    // this block's ids
-    const int S = ((V + C - 1) / C + 31) & ~31, lo = (int)min((long long)V, (long long)rank * S), hi = (int)min((long long)V, (long long)lo + S);
+    if (C > 1) cluster.barrier_wait();
+    const int S = ((V + C - 1) / C + 31) & ~31;                      // ids of a block
+    auto first_id = [&](int r) { return (int)min((long long)V, (long long)r * S); };
+    const int lo = first_id(rank), hi = first_id(rank + 1);
     int kept = 0, turn = 0;
-    Weights w{a.p + (size_t)row0 * V, a.q ? a.q + (size_t)row0 * V : nullptr, ALL, 0, 0, n};
+    Weights w{a.p + (size_t)row0 * V, a.q ? a.q + (size_t)row0 * V : nullptr, ALL, 0, n, 1.0, 0.0};
     double z = 1.0, total = -1.0;                                    // total: the sum that the last pass over the weights as they are gave; -1: there was none
-    for (int last = 0; n > 0;) {
-        const int c = next_child(sh, n, w.node, last);
-        if (c == n) break;
-        last = c;
-        const double mine = weight_of(sh, w, sh.p_of[c], sh.q_of[c]);
-        if ((double)sh.u[c] * z * (double)sh.q_of[c] < mine) {
-            ++kept;
-            if (rank == 0 && tid == 0) a.path[row0 + kept] = c;
-            const size_t row = (size_t)(row0 + c) * V;
-            w = Weights{a.p + row, a.q ? a.q + row : nullptr, ALL, 0, c, n};
-            z = 1.0;
-            total = -1.0;
-        } else if (a.q) {
-            __syncthreads();                                         // the tests before have read what is written next
-            if (tid == 0) sh.inv[w.m] = 1.0 / z;
-            __syncthreads();
-            w.kind = DRAWN;
-            ++w.m;
-            z = total = sum_all<C>(sh, w, lo, hi, turn);
-            turn ^= 1;
-            if (!(z > 0.0)) break;                                   // nothing is left: no other child is kept
-        } else {
-            if (w.kind == ALL) {
-                w.kind = CHOSEN;
-                total = sum_all<C>(sh, w, lo, hi, turn);
-                turn ^= 1;
+    int last = 0;
+    auto step_to = [&](int c) {
+        ++kept;
+        if (rank == 0 && tid == 0) a.path[row0 + kept] = c;
+        const size_t row = (size_t)(row0 + c) * V;
+        w.p = a.p + row;
+        w.q = a.q ? a.q + row : nullptr;
+        w.kind = ALL;
+        w.node = last = c;
+        w.a = z = 1.0;
+        w.b = 0.0;
+        total = -1.0;
+    };
+    for (bool more = true; n > 0;) {                                 // more: there may be children that can be kept
+        const int c = more ? next_child(sh.parent, n, w.node, last) : n;
+        if (c < n) {
+            last = c;
+            const double mine = w.kind == DRAWN ? left_of(w.a, w.b, sh.p_of[c], sh.q_of[c]) : (double)sh.p_of[c];
+            if ((double)sh.u[c] * z * (double)sh.q_of[c] < mine) {
+                step_to(c);
+                continue;
             }
-            double others = 0.0;                                     // the children behind this one
-            for (int i = lane; i < n; i += 32)
-                if (i > c && sh.parent[i] == w.node) others += sh.p_of[i];
-            z = total + warp_sum64(others);
+            w.kind = a.q ? DRAWN : CHOSEN;
+            w.a /= z;
+            w.b = w.b / z + 1.0;
+        } else {
+            more = false;
+            if (total > 0.0) break;
+            w.kind = ALL;                                            // no rejection at this node, or nothing is left of its row
         }
+        z = total = sum_all<C>(sh, w, lo, hi, turn);
+        turn ^= 1;
+        if (!more) break;
+        if (w.kind == CHOSEN) {
+            const int next = first_kept(sh, w, c, total);
+            if (next < n) step_to(next); else more = false;
+        } else more = total > 0.0;
     }
     if (n > 0) {
-        if (!(total > 0.0)) {                                        // no rejection at this node, or nothing is left of its row
-            w.kind = ALL;
-            w.m = 0;
-            total = sum_all<C>(sh, w, lo, hi, turn);
-            turn ^= 1;
-        }
-        const double target = (double)u_final * total;
-        double upto = 0.0, before = 0.0;
-        int holder = -1;                                             // the block whose ids the running sum passes the target at
-#pragma unroll
-        for (int r = 0; r < C; ++r) {
-            const double next = upto + sh.slot[turn ^ 1][r];
-            if (holder < 0 && target >= 0.0 && next > target) { holder = r; before = upto; }
-            upto = next;
-        }
-        if (rank == max(holder, 0)) {
-            const int token = holder < 0 ? -1 : find_id(sh, w, lo, hi, before, target);
-            if (tid == 0) a.next[b] = token;
+        double target = (double)u_final * total, before = 0.0;
+        const bool drawn = target >= 0.0 && target < total;
+        const int part = drawn ? crossing<C * ACC_NW>(sh.slot[turn ^ 1], before, target) : 0, holder = part / ACC_NW;
+        if (rank == holder) {
+            const int l = first_id(holder), h = first_id(holder + 1), k = part % ACC_NW;
+            const int token = drawn ? find_id(sh, w, part_at(l, h, k), part_at(l, h, k + 1), before, target) : -1;
+            if (drawn ? token >= 0 && lane == 0 : tid == 0) a.next[b] = token;
         }
     } else if (rank == 0 && tid == 0) a.next[b] = -1;
     if (rank == 0 && tid == 0) a.accepted[b] = kept;

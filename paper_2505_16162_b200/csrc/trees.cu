@@ -7,6 +7,24 @@
 
 using namespace knnssd;
 
+namespace {
+
+template <int C> knnssd_status launch_accept(const trees::AcceptArgs &a, cudaStream_t s) {
+    if (C > 8) {                                                     // more blocks a cluster than every device has
+        static bool allowed[kMaxDevices] = {};
+        const int dev = current_device_slot();
+        if (!allowed[dev]) {
+            const ApartFromCapture apart;
+            allowed[dev] = cudaFuncSetAttribute(trees::tree_accept_kernel<C>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+            if (!allowed[dev]) { cudaGetLastError(); return KNNSSD_ERR_CUDA; }
+        }
+    }
+    launch_chained(trees::tree_accept_kernel<C>, dim3(C * a.B), dim3(trees::ACC_NT), 0, s, a);
+    return launched();
+}
+
+}  // namespace
+
 extern "C" {
 
 knnssd_status knnssd_tree_tables(const int *lens_dev, const int *row_start_dev, const int *row_parent_dev, int n_requests, int n_rows, int *row_pos_dev,
@@ -35,8 +53,14 @@ knnssd_status knnssd_tree_accept(const float *p_dev, const float *q_dev_or_null,
         return KNNSSD_ERR_INVALID_ARG;
     if (vocab > KNNSSD_MAX_VOCAB || n_requests > KNNSSD_MAX_REQUESTS) return KNNSSD_ERR_CAPACITY;
     const trees::AcceptArgs a{p_dev, q_dev_or_null, vocab, row_token_dev, row_parent_dev, row_start_dev, n_requests, n_rows, u_accept_dev, u_final_dev, path_dev, n_accepted_dev, next_token_dev};
-    launch_chained(trees::tree_accept_kernel<8>, dim3(8 * n_requests), dim3(trees::ACC_NT), 0, reinterpret_cast<cudaStream_t>(cuda_stream), a);
-    return launched();
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+    switch (trees::blocks_of(n_requests, vocab, sm_count())) {
+    case 16: return launch_accept<16>(a, s);
+    case 8: return launch_accept<8>(a, s);
+    case 4: return launch_accept<4>(a, s);
+    case 2: return launch_accept<2>(a, s);
+    default: return launch_accept<1>(a, s);
+    }
 }
 
 knnssd_status knnssd_tree_agree(const int *row_best_dev, const int *row_token_dev, const int *row_parent_dev, const int *row_start_dev, int n_requests, int n_rows,
