@@ -93,8 +93,8 @@ knnssd_status knnssd_keep_rows(void *const *pools_host, int n_pools, int cache_d
     for (int done = 0; done < n_pools; done += a.n_pools) {
         a.n_pools = std::min(n_pools - done, trees::KEEP_POOLS);
         for (int i = 0; i < a.n_pools; ++i) a.pools[i] = static_cast<uint4 *>(pools_host[done + i]);
-        const long long units = (long long)a.n_pools * n_kv_heads * a.pieces, per = trees::KEEP_NT * trees::KEEP_UNITS;
-        launch_chained(trees::keep_rows_kernel, dim3(n_requests, (unsigned)std::min((units + per - 1) / per, 65535ll)), dim3(trees::KEEP_NT), 0,
+        const long long units = (long long)a.n_pools * n_kv_heads * a.pieces;
+        launch_chained(trees::keep_rows_kernel, dim3(n_requests, (unsigned)std::min((units + trees::KEEP_NT - 1) / trees::KEEP_NT, 65535ll)), dim3(trees::KEEP_NT), 0,
                        reinterpret_cast<cudaStream_t>(cuda_stream), a);
     }
     return launched();

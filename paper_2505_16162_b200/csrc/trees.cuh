@@ -129,8 +129,9 @@ __global__ void __launch_bounds__(AGREE_NT) tree_agree_kernel(const AgreeArgs a)
 // ---- the kept path's K and V -----------------------------------------------------------------------------------------------
 // K and V of row path[j] go from position len + path[j] to len + j, in every pool.  path is ascending, so path[j] >= j: in ascending order no row is overwritten
 // before it is read.  A thread has 16 bytes of a head in some pools and moves them through all of the path's rows, MOVES loads ahead of their stores; threads share
-// nothing.  Every moved value is read and written once: bound by memory, and by latency where few rows move.
-constexpr int KEEP_NT = 256, KEEP_POOLS = 256, KEEP_MOST = 64, MOVES = 4, KEEP_UNITS = 2;
+// nothing.  Every moved value is read and written once: bound by memory, and by latency where few rows move.  With two / four pieces a thread in half / a quarter of the blocks, or two or
+// eight loads ahead, 24 requests of 64 pools of 32 heads (30 MB) take 10 - 17 us for 9.
+constexpr int KEEP_NT = 256, KEEP_POOLS = 256, KEEP_MOST = 64, MOVES = 4;
 struct KeepArgs {
     const int *table, *lens, *row_start, *path;
     int B, R, max_pages, n_pages, page_shift, KV, pieces;            // pieces of 16 bytes of a head
@@ -182,25 +183,17 @@ __global__ void __launch_bounds__(KEEP_NT) keep_rows_kernel(const __grid_constan
         __syncthreads();
         const int c = count, moves = c < 0 ? -1 - c : c;
         if (moves > 0) {
-            for (int u0 = blockIdx.y * KEEP_NT + tid; u0 < units; u0 += KEEP_UNITS * gridDim.y * KEEP_NT) {
-                uint4 *p[KEEP_UNITS];
-#pragma unroll
-                for (int e = 0; e < KEEP_UNITS; ++e) {
-                    const int u = u0 + e * gridDim.y * KEEP_NT, h = u / a.pieces;
-                    p[e] = u < units ? a.pools[h / a.KV] + (h % a.KV) * head + u % a.pieces : nullptr;
-                }
+            for (long long u = blockIdx.y * KEEP_NT + tid; u < units; u += (long long)gridDim.y * KEEP_NT) {
+                const int h = (int)u / a.pieces;
+                uint4 *p = a.pools[h / a.KV] + (h % a.KV) * head + (int)u % a.pieces;
                 for (int m0 = 0; m0 < moves; m0 += MOVES) {
-                    uint4 v[KEEP_UNITS][MOVES];
+                    uint4 v[MOVES];
 #pragma unroll
-                    for (int e = 0; e < KEEP_UNITS; ++e)
+                    for (int m = 0; m < MOVES; ++m)
+                        if (m0 + m < moves) v[m] = p[from[m0 + m]];
 #pragma unroll
-                        for (int m = 0; m < MOVES; ++m)
-                            if (p[e] && m0 + m < moves) v[e][m] = p[e][from[m0 + m]];
-#pragma unroll
-                    for (int e = 0; e < KEEP_UNITS; ++e)
-#pragma unroll
-                        for (int m = 0; m < MOVES; ++m)
-                            if (p[e] && m0 + m < moves) p[e][to[m0 + m]] = v[e][m];
+                    for (int m = 0; m < MOVES; ++m)
+                        if (m0 + m < moves) p[to[m0 + m]] = v[m];
                 }
             }
         }
