@@ -59,6 +59,9 @@ class Batch:
             raise RuntimeError(f"no room for the step: {info}")
         return s
 
+    def attend(self, q, k_pages, v_pages, s):
+        return kb.knnssd_paged_attention(q, k_pages, v_pages, self.table, s["lens"], s["start"])
+
     def forward(self, tokens, s, mask=None, whole_prompts=False):
         """Last hidden states of the rows.  mask: sublayers left out (drafting)."""
         sh, w = self.shape, self.w
@@ -75,7 +78,7 @@ class Batch:
                     o = kb.knnssd_packed_attention(q, k, v, s["start"])
                 else:
                     q = kb.knnssd_rotary_store(qkv, self.cos_sin, s["pos"], s["slot"], k_pages, v_pages)
-                    o = kb.knnssd_paged_attention(q, k_pages, v_pages, self.table, s["lens"], s["start"])
+                    o = self.attend(q, k_pages, v_pages, s)
                 x = x + linear(w["wo"][l], o.view(len(tokens), -1))
             if mask is None or not mask[2 * l + 1]:
                 y = self.norm(x, w["mlp_norm"][l])
