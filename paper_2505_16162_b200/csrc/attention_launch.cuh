@@ -4,6 +4,7 @@
 #include "../../include/knnssd.h"
 #include "host_common.cuh"
 #include "row_attention.cuh"
+#include "short_attention.cuh"
 #include "tensor_attention.cuh"
 #include "tensor_maps.cuh"
 
@@ -45,16 +46,22 @@ inline bool get_parts(Scratch &mem, attn::Args &a, int workers, int rows, int hd
     return true;
 }
 
+// Rows that share a K/V head, up to `most` of them a block's: a.gs of its heads, a.subs blocks for all of them, a.tb new rows.
+inline void share_heads(attn::Args &a, int most) {
+    const int G = a.H / a.KV;
+    a.gs = (G + (G + most - 1) / most - 1) / ((G + most - 1) / most);
+    a.subs = (G + a.gs - 1) / a.gs;
+    a.nvh = a.KV * a.subs;
+    a.tb = most / a.gs;
+}
+
 template <int HD, typename KT, bool PAGED, bool TREE = false> knnssd_status launch_rows(attn::Args a, cudaStream_t s) {
     using Rg = rowattn::Ring<HD, KT>;
     static bool configured[kMaxDevices] = {};
     const auto kernel = rowattn::rows_kernel<HD, KT, PAGED, TREE>;
     if (!allow_smem(kernel, Rg::SMEM, configured)) return KNNSSD_ERR_CUDA;
-    const int G = a.H / a.KV, most = 16;
-    a.gs = (G + (G + most - 1) / most - 1) / ((G + most - 1) / most);
-    a.subs = (G + a.gs - 1) / a.gs;
-    a.nvh = a.KV * a.subs;
-    a.tb = most / a.gs;
+    constexpr int most = 16;
+    share_heads(a, most);
     // An item's beginning and end in positions, and what a warp takes at least: extra 0 / 64 / 256: 9 prompts of 3001 tokens 50 / 42 / 55 us, 8 requests
     // of 5 new rows 56 / 58 / 66; least_run 16 / 32 / 64 / 256: 2 requests of 1851 positions 33 / 24 / 22 / -, one of 96 15 / 15 / 15 / 29.
     a.extra = 64;
@@ -80,11 +87,7 @@ template <int HD, int MODE, bool TREE = false> knnssd_status launch_tensor(attn:
     a.err = attention_err_ptr();
     a.wait_limit = g_wait_limit; a.stop_after = g_stop_after;
     if (!a.err || !allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
-    const int G = a.H / a.KV, most = tcattn::HALF_ROWS;
-    a.gs = (G + (G + most - 1) / most - 1) / ((G + most - 1) / most);
-    a.subs = (G + a.gs - 1) / a.gs;
-    a.nvh = a.KV * a.subs;
-    a.tb = most / a.gs;
+    share_heads(a, tcattn::HALF_ROWS);
     const int ctas = sm_count();
     // An item's beginning and end cost a CTA some 5 to 8 thousand clocks, as much as these positions: with 0 / 384 / 1024, 24 short prompts take
     // 88 / 34 / 33 us and 12000 tokens in 4 prompts 935 / 709 / 750.
@@ -115,6 +118,28 @@ template <int HD, int MODE, bool TREE = false> knnssd_status launch_tensor(attn:
     if (!get_parts(mem, a, ctas, tcattn::ROWS, HD)) return KNNSSD_ERR_CUDA;
     launch_chained(kernel, dim3(ctas), dim3(tcattn::threads_of(MODE == tcattn::COPIED)), L::SMEM, s, a, qm, km, vm);
     launch_chained(attn::merge_kernel<HD, bf16_t, true, tcattn::ROWS>, dim3(ctas - 1, 2 * ((std::min(a.tb, most_rows) * a.gs + 7) / 8)), dim3(256), 0, s, a);
+    return launched();
+}
+
+// Trees over short contexts: whether one block for 16 rows and all positions that the table has room for is the sooner way, by microseconds that were measured.  A block takes 3 and,
+// for 128 positions of 128 dimensions, 0.8 (bf16), 1.45 (fp32 rows, bf16 cache) or 3.6 (fp32; contexts filled two thirds of their tables), one block a processor at a time; the ways that
+// share positions out take 16 or 20 whatever the sizes and then read some 7 GB/ms, half of it where the cache is fp32.  One request of 12 rows, 32 heads and 300 positions
+// 9.7 us for 21; 8 requests 18 for 34; of 700 positions and 40 rows 64 for 46; 4 fp32 heads of 64, one request of 60 positions 5.4 for 16.
+inline bool is_short(attn::Args a, int dtype, int cache_dtype, int hd) {
+    share_heads(a, shortattn::ROWS);
+    const long long positions = (long long)a.max_pages << a.page_shift, tiles = (long long)a.R / a.tb + a.B;
+    if (tiles > 65535 || positions > 4096) return false;
+    const double step = hd / 128.0 * (cache_dtype == 0 ? 3.6 : dtype == 0 ? 1.45 : 0.8), ctas = sm_count();
+    const double own = 3.0 + std::ceil(tiles * a.nvh / ctas) * (3.0 + step * positions / 128.0);
+    const double shared = (dtype == 0 && hd == 64 ? 16.0 : 20.0) + (double)a.B * a.KV * positions * hd * (cache_dtype == 0 ? 16.0 : 4.0) / 7e6;
+    return own < shared;
+}
+template <int HD, typename QT, typename KT> knnssd_status launch_short(attn::Args a, cudaStream_t s) {
+    static bool configured[kMaxDevices] = {};
+    const auto kernel = shortattn::short_kernel<HD, QT, KT>;
+    if (!allow_smem(kernel, shortattn::smem_bytes<HD>(), configured)) return KNNSSD_ERR_CUDA;
+    share_heads(a, shortattn::ROWS);
+    launch_chained(kernel, dim3(a.nvh, a.R / a.tb + a.B), dim3(shortattn::NT), shortattn::smem_bytes<HD>(), s, a);
     return launched();
 }
 
@@ -158,6 +183,12 @@ knnssd_status paged_attention(const void *q_dev, int dtype, int n_rows, long lon
     a.seen = seen_dev;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
+        if constexpr (TREE)
+            if (is_short(a, dtype, cache_dtype, head_dim)) {
+                if (dtype == 1) return head_dim == 128 ? launch_short<128, bf16_t, bf16_t>(a, s) : launch_short<64, bf16_t, bf16_t>(a, s);
+                if (head_dim == 128) return cache_dtype == 0 ? launch_short<128, float, float>(a, s) : launch_short<128, float, bf16_t>(a, s);
+                return cache_dtype == 0 ? launch_short<64, float, float>(a, s) : launch_short<64, float, bf16_t>(a, s);
+            }
         if (dtype == 1) {
             const int most_rows = max_fresh > 0 ? std::min(max_fresh, a.R) : a.R;
             // a coordinate of the TMA has 31 bits

@@ -105,6 +105,10 @@ class Trees(Paged):
         return kb.knnssd_tree_attention(q, self.k, self.v, self.table, self.dlens, self.start, self.words, **kw)
 
 
+def _wider(table, by):
+    return torch.cat([table, torch.full((table.shape[0], by), -1, **I32)], dim=1).contiguous()
+
+
 # (lengths held, rows and how far back their parents lie, of each request)
 LENGTHS = [
     ([0], [(1, 1)]), ([95], [(13, 4)]), ([0], [(64, 20)]), ([15], [(30, 0)]), ([1280], [(25, 5)]), ([63], [(64, 63)]),
@@ -119,22 +123,26 @@ LENGTHS = [
 def test_trees_over_pages(kb, dtype, cache, H, KV, hd, at):
     lens, rows = LENGTHS[at]
     rng = np.random.default_rng(50 + at)
-    p = Trees(kb, 7 * at + H, lens, [_parents(rng, *r) for r in rows], KV, hd, (16, 32, 64, 128)[(at + H) % 4], cache)
+    page = (16, 32, 64, 128)[(at + H) % 4]
+    p = Trees(kb, 7 * at + H, lens, [_parents(rng, *r) for r in rows], KV, hd, page, cache)
     q = p.q(H, hd, dtype)
     want, tol = p.want(q)
-    for hint in (0, max(p.fresh)):
-        _check(p.run(kb, q, max_fresh=hint), want, tol, f"max_fresh {hint}")
+    for wide in (p.table, _wider(p.table, 5000 // page)):            # tables with room for short contexts, and for long ones
+        p.table = wide
+        for hint in (0, max(p.fresh)):
+            _check(p.run(kb, q, max_fresh=hint), want, tol, f"{wide.shape[1]} pages, max_fresh {hint}")
 
 
 @pytest.mark.parametrize("dtype,cache", KINDS)
 @pytest.mark.parametrize("H,KV,hd,page", [(4, 2, 64, 16), (10, 2, 128, 64), (3, 3, 128, 16)])
-def test_words_of_all_kinds(kb, dtype, cache, H, KV, hd, page):
+@pytest.mark.parametrize("more", [0, 5000])
+def test_words_of_all_kinds(kb, dtype, cache, H, KV, hd, page, more):
     """Words that come of no tree: none of 64, one, all but its own, random ones; rows of a short request that see nothing."""
     rng = np.random.default_rng(H)
     lens, fresh = [0, 20, 200, 1000, 0], [7, 40, 150, 3, 64]
     kinds = [lambda i: 0, lambda i: 1, lambda i: (1 << 64) - 2, lambda i: int(rng.integers(0, 1 << 63)) * 2 + int(rng.integers(0, 2)), lambda i: 1 << 63, lambda i: 1 << (i % 64)]
     words = [[kinds[(i + b) % len(kinds)](i) for i in range(n)] for b, n in enumerate(fresh)]
-    p = Trees(kb, 3, lens, [[-1] * n for n in fresh], KV, hd, page, cache, words=words)
+    p = Trees(kb, 3, lens, [[-1] * n for n in fresh], KV, hd, page, cache, words=words, wide=2 + more // page)
     q = p.q(H, hd, dtype)
     want, tol = p.want(q)
     got = p.run(kb, q)
@@ -145,9 +153,13 @@ def test_words_of_all_kinds(kb, dtype, cache, H, KV, hd, page):
 @pytest.mark.parametrize("dtype,cache", KINDS)
 @pytest.mark.parametrize("lens,fresh", [([300, 0, 77], [5, 64, 200]), ([20011], [1]), ([40] * 300, [3] * 300)])
 def test_chains_are_the_rows_of_paged_attention(kb, dtype, cache, lens, fresh):
-    p = Trees(kb, 9, lens, [list(range(-1, n - 1)) for n in fresh], 2, 128, 16, cache)
-    q = p.q(6, 128, dtype)
-    assert torch.equal(p.run(kb, q), Paged.run(p, kb, q))
+    """To the bit where the table has room for long contexts; short ones have a kernel of their own."""
+    for wide in (300, 2):
+        p = Trees(kb, 9, lens, [list(range(-1, n - 1)) for n in fresh], 2, 128, 16, cache, wide=wide)
+        q = p.q(6, 128, dtype)
+        got = p.run(kb, q)
+        assert wide == 2 or torch.equal(got, Paged.run(p, kb, q))
+        _check(got, *p.want(q))
 
 
 @pytest.mark.parametrize("dtype,cache", KINDS)
@@ -171,10 +183,11 @@ def test_many_requests_of_all_lengths(kb, dtype, cache):
 @pytest.mark.parametrize("dtype,cache", KINDS)
 @pytest.mark.parametrize("lens,rows", [([33], [(20, 4)]), ([130, 2], [(64, 9), (64, 0)]), ([700], [(64, 30)])])
 @pytest.mark.parametrize("page", [16, 64])
-def test_what_is_not_finite_reaches_only_rows_that_see_it(kb, dtype, cache, lens, rows, page):
+@pytest.mark.parametrize("more", [0, 5000])
+def test_what_is_not_finite_reaches_only_rows_that_see_it(kb, dtype, cache, lens, rows, page, more):
     """Siblings' K and V, and the rows' that a row has behind it, play no part whatever they are."""
     rng = np.random.default_rng(8)
-    p = Trees(kb, 13, lens, [_parents(rng, *r) for r in rows], 2, 128, page, cache)
+    p = Trees(kb, 13, lens, [_parents(rng, *r) for r in rows], 2, 128, page, cache, wide=2 + more // page)
     for b, (a, n) in enumerate(zip(lens, p.fresh)):
         for i, val in ((n // 2, torch.inf), (n - 2, torch.nan), (3, -torch.inf)):
             at, off = int(p.table[b, (a + i) // page]), (a + i) % page
@@ -197,9 +210,10 @@ def test_what_is_not_finite_reaches_only_rows_that_see_it(kb, dtype, cache, lens
 
 
 @pytest.mark.parametrize("dtype,cache", KINDS)
-def test_pages_that_are_gone(kb, dtype, cache):
+@pytest.mark.parametrize("wide", [2, 300])
+def test_pages_that_are_gone(kb, dtype, cache, wide):
     rng = np.random.default_rng(4)
-    p = Trees(kb, 11, [40, 100, 0], [_parents(rng, 30, 5), _parents(rng, 64, 9), _parents(rng, 20, 2)], 2, 64, 16, cache)
+    p = Trees(kb, 11, [40, 100, 0], [_parents(rng, 30, 5), _parents(rng, 64, 9), _parents(rng, 20, 2)], 2, 64, 16, cache, wide=wide)
     gone = {0: range(0, 99), 1: (0, 6, 7), 2: (0,)}
     for b, cols in gone.items():
         for c in cols:
@@ -227,9 +241,10 @@ def test_a_tree_level_by_level(kb, dtype, cache):
         _check(got, want[rows], tol[rows], f"rows {a} .. {z - 1}")
 
 
-def test_rows_of_nobody_and_strides(kb):
+@pytest.mark.parametrize("wide", [2, 300])
+def test_rows_of_nobody_and_strides(kb, wide):
     rng = np.random.default_rng(6)
-    p = Trees(kb, 19, [64, 5], [_parents(rng, 9, 3), _parents(rng, 4, 2)], 2, 64, 32, "bf16")
+    p = Trees(kb, 19, [64, 5], [_parents(rng, 9, 3), _parents(rng, 4, 2)], 2, 64, 32, "bf16", wide=wide)
     wide = torch.randn(20, 6 * 64 + 72, device="cuda").bfloat16()
     q = wide[:, 8:8 + 6 * 64].unflatten(1, (6, 64))
     p.words = torch.cat([torch.full((3,), -1, dtype=torch.int64, device="cuda"), p.words, torch.full((4,), -1, dtype=torch.int64, device="cuda")])
@@ -244,9 +259,10 @@ def test_rows_of_nobody_and_strides(kb):
 
 
 @pytest.mark.parametrize("dtype,cache", KINDS)
-def test_lengths_out_of_range_stay_inside_the_pool(kb, dtype, cache):
+@pytest.mark.parametrize("wide", [2, 300])
+def test_lengths_out_of_range_stay_inside_the_pool(kb, dtype, cache, wide):
     rng = np.random.default_rng(1)
-    p = Trees(kb, 23, [40, 10, 30], [_parents(rng, 8, 3) for _ in range(3)], 2, 64, 16, cache)
+    p = Trees(kb, 23, [40, 10, 30], [_parents(rng, 8, 3) for _ in range(3)], 2, 64, 16, cache, wide=wide)
     q = p.q(4, 64, dtype)
     want, tol = p.want(q)
     p.k.nan_to_num_()
