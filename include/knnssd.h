@@ -452,7 +452,7 @@ knnssd_status knnssd_rotary_store(const void *qkv_dev, int dtype, int n_rows, lo
  *   max_fresh  the most rows a request has in this call, 0 if the host does not know: the size of a launch goes by it, never the result
  *              (negative: KNNSSD_ERR_INVALID_ARG)
  *   scale      finite and not negative, else KNNSSD_ERR_INVALID_ARG; 0 gives equal weights
- *   n_rows * n_heads below 2^31, else KNNSSD_ERR_CAPACITY
+ *   n_rows * n_heads below 2^31, of bf16 rows n_pages * n_kv_heads * page_size up to 2^34, else KNNSSD_ERR_CAPACITY
  * Positions whose page id is outside [0, n_pages) are not seen; a row that sees nothing gives zeros, and so do rows before row_start[0] and from
  * row_start[n_requests] on.  What a row does not see never reaches it, not even NaN; what it sees and is not finite counts as in IEEE arithmetic (a score of
  * NaN or +inf makes the row NaN, one of -inf has no weight).  Such calls are slower, up to some hundred times.  Values so large that a sum of weights times

@@ -80,10 +80,10 @@ template <int HD, typename KT, bool PAGED, bool TREE = false> knnssd_status laun
 }
 
 // most_rows: the rows that a request is believed to have at most.
-template <int HD, int MODE, bool TREE = false> knnssd_status launch_tensor(attn::Args a, int most_rows, cudaStream_t s) {
+template <int HD, bool PAGED, bool TREE = false> knnssd_status launch_tensor(attn::Args a, int most_rows, cudaStream_t s) {
     using L = tcattn::Lay<HD>;
     static bool configured[kMaxDevices] = {};
-    const auto kernel = tcattn::tensor_kernel<HD, MODE, TREE>;
+    const auto kernel = tcattn::tensor_kernel<HD, PAGED, TREE>;
     a.err = attention_err_ptr();
     a.wait_limit = g_wait_limit; a.stop_after = g_stop_after;
     if (!a.err || !allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
@@ -103,12 +103,12 @@ template <int HD, int MODE, bool TREE = false> knnssd_status launch_tensor(attn:
     const cuuint64_t qs[3] = {HD, (cuuint64_t)a.H, (cuuint64_t)a.R}, qst[2] = {HD * 2, (cuuint64_t)a.q_stride * 2};
     const cuuint32_t qb[3] = {64, (cuuint32_t)a.gs, (cuuint32_t)a.tb};
     bool made = bf16_map(&qm, a.q, 3, qs, qst, qb);
-    if (MODE == tcattn::TILED) {
+    if (PAGED) {                                                     // groups of eight rows, the rows' 64 dimensions apart from one another
         const int page = 1 << a.page_shift;
-        const cuuint64_t ks[2] = {HD, (cuuint64_t)a.n_pages * a.KV * page}, kst[1] = {HD * 2};
-        const cuuint32_t kb[2] = {64, (cuuint32_t)(page < tcattn::KEYS ? page : tcattn::KEYS)};
-        made = made && bf16_map(&km, a.k, 2, ks, kst, kb) && bf16_map(&vm, a.v, 2, ks, kst, kb);
-    } else if (MODE == tcattn::PACKED) {
+        const cuuint64_t ks[4] = {64, 8, HD / 64, (cuuint64_t)a.n_pages * a.KV * page / 8}, kst[3] = {HD * 2, 128, HD * 16};
+        const cuuint32_t kb[4] = {64, 8, HD / 64, (cuuint32_t)(page < tcattn::PIECE ? page : tcattn::PIECE) / 8};
+        made = made && bf16_map(&km, a.k, 4, ks, kst, kb) && bf16_map(&vm, a.v, 4, ks, kst, kb);
+    } else {
         const cuuint64_t ks[3] = {HD, (cuuint64_t)a.KV, (cuuint64_t)a.R}, kst[2] = {HD * 2, (cuuint64_t)a.k_stride * 2}, vst[2] = {HD * 2, (cuuint64_t)a.v_stride * 2};
         const cuuint32_t kb[3] = {64, 1, tcattn::KEYS};
         made = made && bf16_map(&km, a.k, 3, ks, kst, kb) && bf16_map(&vm, a.v, 3, ks, vst, kb);
@@ -116,7 +116,7 @@ template <int HD, int MODE, bool TREE = false> knnssd_status launch_tensor(attn:
     if (!made) return KNNSSD_ERR_CUDA;
     Scratch mem(s);
     if (!get_parts(mem, a, ctas, tcattn::ROWS, HD)) return KNNSSD_ERR_CUDA;
-    launch_chained(kernel, dim3(ctas), dim3(tcattn::threads_of(MODE == tcattn::COPIED)), L::SMEM, s, a, qm, km, vm);
+    launch_chained(kernel, dim3(ctas), dim3(tcattn::threads_of(PAGED)), L::SMEM, s, a, qm, km, vm);
     launch_chained(attn::merge_kernel<HD, bf16_t, true, tcattn::ROWS>, dim3(ctas - 1, 2 * ((std::min(a.tb, most_rows) * a.gs + 7) / 8)), dim3(256), 0, s, a);
     return launched();
 }
@@ -191,10 +191,9 @@ knnssd_status paged_attention(const void *q_dev, int dtype, int n_rows, long lon
             }
         if (dtype == 1) {
             const int most_rows = max_fresh > 0 ? std::min(max_fresh, a.R) : a.R;
-            // a coordinate of the TMA has 31 bits
-            if (page_size >= 64 && (long long)n_pages * page_size * n_kv_heads <= INT_MAX)
-                return head_dim == 128 ? launch_tensor<128, tcattn::TILED, TREE>(a, most_rows, s) : launch_tensor<64, tcattn::TILED, TREE>(a, most_rows, s);
-            return head_dim == 128 ? launch_tensor<128, tcattn::COPIED, TREE>(a, most_rows, s) : launch_tensor<64, tcattn::COPIED, TREE>(a, most_rows, s);
+            // a coordinate of the copies, eight rows, has 31 bits
+            if ((long long)n_pages * n_kv_heads > INT_MAX / (page_size / 8)) return KNNSSD_ERR_CAPACITY;
+            return head_dim == 128 ? launch_tensor<128, true, TREE>(a, most_rows, s) : launch_tensor<64, true, TREE>(a, most_rows, s);
         }
         if (head_dim == 128) return cache_dtype == 0 ? launch_rows<128, float, true, TREE>(a, s) : launch_rows<128, bf16_t, true, TREE>(a, s);
         return cache_dtype == 0 ? launch_rows<64, float, true, TREE>(a, s) : launch_rows<64, bf16_t, true, TREE>(a, s);

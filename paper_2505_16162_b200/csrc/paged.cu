@@ -108,7 +108,7 @@ knnssd_status knnssd_packed_attention(const void *q_dev, const void *k_dev, cons
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if (dtype == 1) {
-            return head_dim == 128 ? launch_tensor<128, tcattn::PACKED>(a, a.R, s) : launch_tensor<64, tcattn::PACKED>(a, a.R, s);
+            return head_dim == 128 ? launch_tensor<128, false>(a, a.R, s) : launch_tensor<64, false>(a, a.R, s);
         }
         return head_dim == 128 ? launch_rows<128, float, false>(a, s) : launch_rows<64, float, false>(a, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }

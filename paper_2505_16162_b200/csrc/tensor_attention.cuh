@@ -3,7 +3,7 @@
 // The mathematics is the rows kernel's.  A block of a launch (one per SM) takes two halves of 128 rows (query heads that share a K/V head times
 // new rows) through the positions, in tiles of 128 and steps of 64:
 //
-//   warp 8       brings q, K and V in, a ring of tiles ahead of the products (K and V of pages: three more warps with it)
+//   warp 8       brings q, K and V in, a ring of tiles ahead of the products (K and V of pages: a second warp with it)
 //   warps 9, 10  issue the products of a half each: S = q K^T into tensor memory, O += P V with P read from tensor memory and V as the
 //                transposed operand straight from its row-major tile
 //   warps 0 - 3  the softmax of the first half, a row per thread: scores out of tensor memory, exponentials, P back as bf16 over them
@@ -39,8 +39,10 @@ namespace tcattn {
 using namespace attn;
 
 constexpr int KEYS = 128, SUB = 64, HALF_ROWS = 128, ROWS = 256;      // positions of a tile, and of a step of the softmax
-constexpr int SOFT_WARPS = 8, LOADERS = 4, LOAD_WARP = 8, MMA_WARP = 9;      // pages: the other loaders are the warps behind the products'
-__host__ __device__ constexpr int threads_of(bool copied) { return (SOFT_WARPS + 2 + (copied ? LOADERS : 1)) * 32; }
+constexpr int SOFT_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9;      // pages: the second loader is the warp behind the products'
+__host__ __device__ constexpr int loaders_of(bool paged) { return paged ? 2 : 1; }
+__host__ __device__ constexpr int threads_of(bool paged) { return (SOFT_WARPS + 2 + loaders_of(paged)) * 32; }
+constexpr int PIECE = KEYS / 2;           // positions of a page that a copy brings at most: both loaders have some of a tile
 constexpr int NCOST = 128;
 constexpr int BAND = KEYS * 128;          // bytes of 64 dimensions of a tile: rows of 128 bytes, swizzled
 constexpr int INFO = 16;                  // steps whose page masks are kept
@@ -53,6 +55,10 @@ constexpr int TMEM_COLS = 512, O_COL = 256;
 
 template <int HD> struct Lay {
     static constexpr int TILE = KEYS * HD * 2, BANDS = HD / 64;
+    // Eight rows of 64 dimensions, 1024 bytes, are what the swizzle turns.  K and V of packed rows lie as the queries, all rows of 64 dimensions and then the next 64; of pages the next
+    // 64 dimensions of eight rows lie behind them, so that one copy brings a page.
+    __host__ __device__ static constexpr int group(bool paged) { return paged ? 1024 * BANDS : 1024; }       // from eight rows to the next
+    __host__ __device__ static constexpr int band(bool paged) { return paged ? 1024 : BAND; }                // from 64 dimensions to the next
     static constexpr int TILES = HD == 128 ? 5 : 10;
     static constexpr int SMEM = (2 + TILES) * TILE + 1024;
 };
@@ -99,9 +105,11 @@ __device__ __forceinline__ uint32_t elect() {
 __device__ __forceinline__ void bar_expect_if(uint32_t b, uint32_t bytes, uint32_t one) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(b), "r"(bytes), "r"(one) : "memory");
 }
-__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar, uint32_t one) {
+// Groups of eight rows from `group` on, all dimensions.
+__device__ __forceinline__ void tma_groups(uint32_t dst, const CUtensorMap *map, int group, uint32_t bar, uint32_t one) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t"
-                 "@p cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}" ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(one)
+                 "@p cp.async.bulk.tensor.4d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %3, %3, %4}], [%2];\n\t}" ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(group),
+                 "r"(one)
                  : "memory");
 }
 __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar, uint32_t one) {
@@ -111,39 +119,54 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int
                  : "memory");
 }
 // Shared-memory operand descriptors, 128-byte swizzle: address / 16 in bits 0 .. 13, leading offset / 16 in 16 .. 29, stride offset / 16 in
-// 32 .. 45, version 1 in 46 .. 47, swizzle mode 2 in 61 .. 63.  Rows are 128 bytes, eight of them (1024 bytes) the stride.  Read along
+// 32 .. 45, version 1 in 46 .. 47, swizzle mode 2 in 61 .. 63.  Rows are 128 bytes, from eight of them to the next the stride.  Read along
 // the dimensions (q, K): the leading offset plays no part.  Read along the positions (V, the transposed operand): it leads to the next 64 dimensions.
 // The constant upper half, and the lower half.
-constexpr uint32_t DESC_UPPER = (1024u >> 4) | (1u << 14) | (2u << 29);
-__device__ __forceinline__ uint32_t desc_of(uint32_t addr) { return (addr >> 4) | ((uint32_t)(BAND >> 4) << 16); }
+__host__ __device__ constexpr uint32_t desc_upper(int group) { return ((uint32_t)group >> 4) | (1u << 14) | (2u << 29); }
+__device__ __forceinline__ uint32_t desc_of(uint32_t addr, int band) { return (addr >> 4) | ((uint32_t)(band >> 4) << 16); }
 // fp32 sums, bf16 operands, M = 128, N columns; transposed: the second operand is read along its rows.
 __host__ __device__ constexpr uint32_t idesc_of(int n, bool transposed) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (transposed ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 // A row of products as one piece of code, so that their operands differ from one another by constants; one thread of the warp issues them.
-#define KNNSSD_SS(K) "add.u32 x, %1, " K ";\n\tadd.u32 y, %2, " K ";\n\tmov.b64 da, {x, %5};\n\tmov.b64 db, {y, %5};\n\t"
-#define KNNSSD_SS_FIRST "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, 0;\n\t"
-#define KNNSSD_SS_NEXT(K) KNNSSD_SS(K) "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, 1;\n\t"
+#define KNNSSD_SS(Q, K) "add.u32 x, %1, " Q ";\n\tadd.u32 y, %2, " K ";\n\tmov.b64 da, {x, %5};\n\tmov.b64 db, {y, %6};\n\t"
+#define KNNSSD_SS_FIRST "{\n\t.reg .pred q;\n\t.reg .b64 da, db;\n\t.reg .b32 x, y;\n\telect.sync _|q, 0xffffffff;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %6};\n\t" \
+    "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, 0;\n\t"
+#define KNNSSD_SS_NEXT(Q, K) KNNSSD_SS(Q, K) "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, 1;\n\t"
+#define KNNSSD_SS_LAST "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t}"
 // S (128 x 64) = q k^T over HD dimensions: steps of 16 are 32 bytes apart, the second 64 dimensions a band further; then bar is told.
-template <int HD> __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t q, uint32_t k, uint32_t idesc, uint32_t bar) {
-    if constexpr (HD == 128)
-        asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 da, db;\n\t.reg .b32 x, y;\n\telect.sync _|q, 0xffffffff;\n\t" KNNSSD_SS_FIRST KNNSSD_SS_NEXT("2") KNNSSD_SS_NEXT("4")
-                     KNNSSD_SS_NEXT("6") KNNSSD_SS_NEXT("1024") KNNSSD_SS_NEXT("1026") KNNSSD_SS_NEXT("1028") KNNSSD_SS_NEXT("1030")
-                     "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t}" ::"r"(d), "r"(q), "r"(k), "r"(idesc), "r"(bar), "r"(DESC_UPPER)
+template <int HD, bool PAGED> __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t q, uint32_t k, uint32_t idesc, uint32_t bar) {
+    constexpr uint32_t q_upper = desc_upper(1024), k_upper = desc_upper(Lay<HD>::group(PAGED));
+    static_assert(BAND >> 4 == 1024, "as written below");
+    if constexpr (HD == 128 && PAGED)
+        asm volatile(KNNSSD_SS_FIRST KNNSSD_SS_NEXT("2", "2") KNNSSD_SS_NEXT("4", "4") KNNSSD_SS_NEXT("6", "6") KNNSSD_SS_NEXT("1024", "64") KNNSSD_SS_NEXT("1026", "66")
+                     KNNSSD_SS_NEXT("1028", "68") KNNSSD_SS_NEXT("1030", "70") KNNSSD_SS_LAST ::"r"(d), "r"(q), "r"(k), "r"(idesc), "r"(bar), "r"(q_upper), "r"(k_upper)
+                     : "memory");
+    else if constexpr (HD == 128)
+        asm volatile(KNNSSD_SS_FIRST KNNSSD_SS_NEXT("2", "2") KNNSSD_SS_NEXT("4", "4") KNNSSD_SS_NEXT("6", "6") KNNSSD_SS_NEXT("1024", "1024") KNNSSD_SS_NEXT("1026", "1026")
+                     KNNSSD_SS_NEXT("1028", "1028") KNNSSD_SS_NEXT("1030", "1030") KNNSSD_SS_LAST ::"r"(d), "r"(q), "r"(k), "r"(idesc), "r"(bar), "r"(q_upper), "r"(k_upper)
                      : "memory");
     else
-        asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 da, db;\n\t.reg .b32 x, y;\n\telect.sync _|q, 0xffffffff;\n\t" KNNSSD_SS_FIRST KNNSSD_SS_NEXT("2") KNNSSD_SS_NEXT("4")
-                     KNNSSD_SS_NEXT("6") "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t}" ::"r"(d), "r"(q), "r"(k), "r"(idesc), "r"(bar),
-                     "r"(DESC_UPPER)
+        asm volatile(KNNSSD_SS_FIRST KNNSSD_SS_NEXT("2", "2") KNNSSD_SS_NEXT("4", "4") KNNSSD_SS_NEXT("6", "6") KNNSSD_SS_LAST ::"r"(d), "r"(q), "r"(k), "r"(idesc), "r"(bar),
+                     "r"(q_upper), "r"(k_upper)
                      : "memory");
 }
 #define KNNSSD_TS_NEXT(A, B) "add.u32 x, %1, " A ";\n\tadd.u32 y, %2, " B ";\n\tmov.b64 db, {y, %5};\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %3, 1;\n\t"
-// O (128 x HD) += P V over 64 positions: P 8 columns a step of 16, V 2048 bytes.  add 0: the first product begins the sum.  Then bar is told.
-__device__ __forceinline__ void mma_values(uint32_t d, uint32_t p, uint32_t v, uint32_t idesc, uint32_t add, uint32_t bar) {
-    asm volatile("{\n\t.reg .pred q, a;\n\t.reg .b64 db;\n\t.reg .b32 x, y;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 a, %4, 0;\n\tmov.b64 db, {%2, %5};\n\t"
-                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, a;\n\t" KNNSSD_TS_NEXT("8", "128") KNNSSD_TS_NEXT("16", "256") KNNSSD_TS_NEXT("24", "384")
-                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t}" ::"r"(d), "r"(p), "r"(v), "r"(idesc), "r"(add), "r"(DESC_UPPER), "r"(bar)
-                 : "memory");
+#define KNNSSD_TS_FIRST "{\n\t.reg .pred q, a;\n\t.reg .b64 db;\n\t.reg .b32 x, y;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 a, %4, 0;\n\tmov.b64 db, {%2, %5};\n\t" \
+    "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, a;\n\t"
+#define KNNSSD_TS_LAST "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t}"
+// O (128 x HD) += P V over 64 positions: P 8 columns a step of 16, V two groups of eight rows.  add 0: the first product begins the sum.  Then bar is told.
+template <int HD, bool PAGED> __device__ __forceinline__ void mma_values(uint32_t d, uint32_t p, uint32_t v, uint32_t idesc, uint32_t add, uint32_t bar) {
+    constexpr int group = Lay<HD>::group(PAGED);
+    static_assert(group == 1024 || group == 2048, "as written below");
+    if constexpr (group == 2048)
+        asm volatile(KNNSSD_TS_FIRST KNNSSD_TS_NEXT("8", "256") KNNSSD_TS_NEXT("16", "512") KNNSSD_TS_NEXT("24", "768") KNNSSD_TS_LAST ::"r"(d), "r"(p), "r"(v), "r"(idesc), "r"(add),
+                     "r"(desc_upper(group)), "r"(bar)
+                     : "memory");
+    else
+        asm volatile(KNNSSD_TS_FIRST KNNSSD_TS_NEXT("8", "128") KNNSSD_TS_NEXT("16", "256") KNNSSD_TS_NEXT("24", "384") KNNSSD_TS_LAST ::"r"(d), "r"(p), "r"(v), "r"(idesc), "r"(add),
+                     "r"(desc_upper(group)), "r"(bar)
+                     : "memory");
 }
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
@@ -239,9 +262,6 @@ __device__ __forceinline__ void turn4(uint4 (&v)[4], int lane) {
     swap(v[1], v[3], 2);
 }
 
-// Where K and V come from: packed rows; pages by 16-byte copies; pages of 64 positions or more by TMA.
-enum { PACKED = 0, COPIED = 1, TILED = 2 };
-
 // What a run has of an item: n[h] steps of SUB positions from tile j0 on for either half; a half without rows, or whose rows end before, has none.
 struct Job {
     int from, to, j0, n[2], tiles, seen0, tokens;
@@ -334,17 +354,19 @@ template <int HD> __device__ __noinline__ void spoil_rows(const Args &a, const C
     } while (it.next(a) && it.start < x1);
 }
 
-template <int HD, int MODE, bool TREE = false>
-__global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+// K and V come from pages or from packed rows.
+template <int HD, bool PAGED, bool TREE = false>
+__global__ void __launch_bounds__(threads_of(PAGED), 1) tensor_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                                                         const __grid_constant__ CUtensorMap vmap) {
     using L = Lay<HD>;
-    constexpr bool PAGED = MODE != PACKED;
+    constexpr int GROUP = L::group(PAGED), NEXT_BAND = L::band(PAGED);
     extern __shared__ unsigned char raw[];
     __shared__ Costs<NCOST> costs;
     __shared__ uint64_t bars[2 + 2 + 2 * L::TILES + 4 + 4 + 4 + 2];    // s_full, p_full and o_full: [half][buffer]
     __shared__ uint32_t tmem_base;
     __shared__ volatile int quit, odd;                               // a wait gave up; some row is not finite
     __shared__ volatile unsigned info[INFO];                         // the 16-position groups of a step's tile that have a page
+    __shared__ volatile unsigned filled[2];                          // tiles that a loader has filled its part of, when it is done
     const uint32_t smem = (smem_addr(raw) + 1023u) & ~1023u, q_tile = smem, ring = smem + 2 * L::TILE;
     const uint32_t q_full = smem_addr(bars), q_empty = q_full + 16, kv_full = q_empty + 16, kv_empty = kv_full + 8 * L::TILES, s_full = kv_empty + 8 * L::TILES,
                    p_full = s_full + 32, o_full = p_full + 32, all_done = o_full + 32;
@@ -355,7 +377,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
             bar_init(q_full + 8 * i, 1); bar_init(q_empty + 8 * i, 1); bar_init(all_done + 8 * i, 1);
             for (int b = 0; b < 2; ++b) { bar_init(o_full + 8 * (2 * i + b), 1); bar_init(s_full + 8 * (2 * i + b), 2); bar_init(p_full + 8 * (2 * i + b), 4); }
         }
-        for (int i = 0; i < L::TILES; ++i) { bar_init(kv_full + 8 * i, MODE == COPIED ? LOADERS * 32 + 1 : 1); bar_init(kv_empty + 8 * i, 2); }
+        for (int i = 0; i < L::TILES; ++i) { bar_init(kv_full + 8 * i, loaders_of(PAGED)); bar_init(kv_empty + 8 * i, 2); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
@@ -380,14 +402,13 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
 
         if (warp == LOAD_WARP || warp >= MMA_WARP + 2) {
             // ---- copies ------------------------------------------------------------------------------------------------
-            // Packed rows come by TMA, one copy for 64 dimensions of a tile.  A tile of pages of 16 positions would be 16 copies, and a copy takes the issuing
-            // warp some 100 clocks: such pages come by 16-byte asynchronous copies of four warps, laid out as the TMA would.  64 single tokens over
-            // pages of 16 / 32 / 64 / 128 positions: by TMA 171 / 131 / 117 / 115 us, by copies 137 / - / - / 133.  What no row of the block sees, and
-            // what has no page, becomes zeros.
-            const int loader = warp == LOAD_WARP ? 0 : warp - MMA_WARP - 1;
+            // By TMA: packed rows one copy for 64 dimensions of a tile; pages one copy for each of a tile's, two of the larger ones, shared out between two warps, since a copy takes the
+            // issuing warp some 100 clocks: 64 requests of 16 rows over pages of 16 / 32 / 64 / 128 positions 134 / 128 / 126 / 124 us, by one warp 171 / 138 / 129 / 128, by 16-byte
+            // copies of four warps 146 whatever the pages.  What has no page is not copied.
+            const int loader = warp == LOAD_WARP ? 0 : 1;
             const uint32_t one = elect();
             unsigned fills = 0, slot = 0, turn_of = 0, qfills[2] = {0, 0}, step0 = 0;      // slot, turn_of: the ring's next tile
-            const int piece = MODE == COPIED ? 16 : min(1 << a.page_shift, KEYS), pieces = KEYS / piece;
+            const int piece = min(1 << a.page_shift, PIECE), pieces = KEYS / piece;
             int id = -1, next_id = -1;                               // pages: lane i: the page of piece i of the tile, of the one behind it
             auto page_of = [&](int j) {
                 const int pos = j * KEYS + lane * piece;
@@ -395,11 +416,6 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 const int p = __ldg(a.table + (size_t)it.b * a.max_pages + (pos >> a.page_shift));
                 return p < a.n_pages ? p : -1;
             };
-            constexpr int CH = HD / 8, PER = 32 / CH, N = 16 / PER;  // 16-byte pieces of a position; positions a copy of the warp; copies for 16
-            const int chunk = lane % CH, sub = lane / CH;
-            uint32_t turned[8 / PER];                                // where the swizzle puts this lane's piece of its positions, modulo 8
-#pragma unroll
-            for (int n = 0; n < 8 / PER; ++n) turned[n] = ((chunk & 7) ^ (n * PER + sub)) << 4;
             while (more && ok) {
                 const Job job(a, it, x0, x1);
                 // tiles in the order of their use (see the products)
@@ -448,48 +464,16 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                         info[(step0 + t) % INFO] = groups;
                     }
                     if (PAGED && ahead && (second || !own)) { id = next_id; next_id = page_of(job.j0 + t + 1); }
-                    if (MODE == COPIED) {
-                        const unsigned char *pool = static_cast<const unsigned char *>(is_k ? a.k : a.v);
-                        const uint32_t at = dst + (chunk >> 3) * BAND + sub * 128;
-#pragma unroll 2
-                        for (int g = loader; g < KEYS / 16; g += LOADERS) {
-                            const int pg = __shfl_sync(0xffffffffu, page, g), pos = (job.j0 + t) * KEYS + 16 * g;
-                            const int seen = pg >= 0 ? it.kv - pos - sub : 0;       // positions from this lane's first on that count
-                            const unsigned char *src =
-                                pool + ((((size_t)max(pg, 0) * a.KV + kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) + sub) * (HD * 2) + chunk * 16;
-                            const uint32_t to = at + g * 2048;
-                            if (__all_sync(0xffffffffu, seen >= 16)) {
-#pragma unroll
-                                for (int n = 0; n < N; ++n)
-                                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + n * PER * 128 + turned[n % (8 / PER)]), "l"(src + n * PER * (HD * 2)) : "memory");
-                            } else {
-#pragma unroll 1
-                                for (int n = 0; n < N; ++n) {
-                                    const int row = n * PER, size = row < seen ? 16 : 0;
-                                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + row * 128 + (((chunk & 7) ^ ((row + sub) & 7)) << 4)),
-                                                 "l"(size ? src + row * (HD * 2) : pool), "r"(size)
-                                                 : "memory");
-                                }
-                            }
-                        }
-                        // The barrier has an arrival of each lane when its copies so far have landed, and one that hands on the note.
-                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-                        if (loader == 0 && lane == 0) bar_arrive(bar);
-                    } else if (MODE == TILED) {
-                        const CUtensorMap *map = is_k ? &kmap : &vmap;
+                    const CUtensorMap *map = is_k ? &kmap : &vmap;
+                    if (PAGED) {
                         __syncwarp();                                // behind the note: the arrival that goes with it hands it on
-                        bar_expect_if(bar, __popc(there) * piece * HD * 2, one);
-                        const int y = ((page * a.KV + kvh) << a.page_shift) + (((job.j0 + t) * KEYS + lane * piece) & ((1 << a.page_shift) - 1));
-                        for (int g = 0; g < pieces; ++g) {
-                            const int yg = __shfl_sync(0xffffffffu, y, g);
-#pragma unroll
-                            for (int b = 0; b < L::BANDS; ++b) tma_2d(dst + b * BAND + g * piece * 128, map, 64 * b, yg, bar, there >> g & one);
-                        }
+                        bar_expect_if(bar, __popc(there & (0x55555555u << loader)) * piece * HD * 2, one);
+                        const int group = (((page * a.KV + kvh) << (a.page_shift - 3))) + ((((job.j0 + t) * KEYS + lane * piece) & ((1 << a.page_shift) - 1)) >> 3);
+                        for (int g = loader; g < pieces; g += 2) tma_groups(dst + g * piece * HD * 2, map, __shfl_sync(0xffffffffu, group, g), bar, there >> g & one);
                     } else {
-                        const CUtensorMap *map = is_k ? &kmap : &vmap;
                         bar_expect_if(bar, L::TILE, one);
 #pragma unroll
-                        for (int b = 0; b < L::BANDS; ++b) tma_3d(dst + b * BAND, map, 64 * b, kvh, it.r.row0 + (job.j0 + t) * KEYS, bar, one);
+                        for (int b = 0; b < L::BANDS; ++b) tma_3d(dst + b * NEXT_BAND, map, 64 * b, kvh, it.r.row0 + (job.j0 + t) * KEYS, bar, one);
                     }
                     ++fills;
                     if (++slot == L::TILES) { slot = 0; ++turn_of; }
@@ -498,13 +482,18 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 step0 += T;
                 more = it.next(a) && it.start < x1;
             }
-            if (MODE == COPIED) asm volatile("cp.async.wait_all;" ::: "memory");
+            if (PAGED) {                                             // where one loader gave up the other's tiles still have to be full: it arrives for those that it left out
+                if (lane == 0) filled[loader] = fills;
+                asm volatile("bar.sync 1, 64;" ::: "memory");
+                const unsigned all = max(filled[0], filled[1]);
+                for (; fills < all; ++fills)
+                    if (lane == 0) bar_arrive(kv_full + 8 * (fills % L::TILES));
+            }
             // every copy has landed and every product has let go of its tile before the block goes
-            for (unsigned i = loader ? fills : fills > L::TILES ? fills - L::TILES : 0; i < fills; ++i) {
+            for (unsigned i = fills > L::TILES ? fills - L::TILES : 0; i < fills; ++i) {
                 const unsigned slot = i % L::TILES, parity = i / L::TILES & 1;
                 if (ok) ok = warp_wait(kv_empty + 8 * slot, parity, &quit, a, 203);
-                if (MODE != COPIED && !ok)
-                    bar_settle(kv_full + 8 * slot, parity);
+                if (!ok) bar_settle(kv_full + 8 * slot, parity);
             }
             for (int h = 0; h < 2; ++h)
                 if (qfills[h]) {
@@ -515,9 +504,9 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
             // ---- products ------------------------------------------------------------------------------------------------
             // A warp per half: its own instructions, some 150 a step next to 640 clocks of products, bound the loop where one warp served both.
             // Of the half two steps are under way: while the softmax works on one, the scores of the other are formed.
-            constexpr uint32_t S_DESC = idesc_of(SUB, false), O_DESC = idesc_of(HD, true), SUB_STEP = SUB * 128 >> 4;
+            constexpr uint32_t S_DESC = idesc_of(SUB, false), O_DESC = idesc_of(HD, true), SUB_STEP = SUB / 8 * GROUP >> 4;
             const int h = warp - MMA_WARP;
-            const uint32_t q_desc = desc_of(q_tile + h * L::TILE), s_col = tmem + h * KEYS, o_col = tmem + O_COL + h * HD;
+            const uint32_t q_desc = desc_of(q_tile + h * L::TILE, BAND), s_col = tmem + h * KEYS, o_col = tmem + O_COL + h * HD;
             const uint32_t my_s = s_full + 16 * h, my_p = p_full + 16 * h, my_o = o_full + 16 * h, my_q = q_full + 8 * h, my_q_empty = q_empty + 8 * h;
             unsigned slot = 0, phase = 0, q_phase = 0, step0 = 0;    // slot, phase: the ring's next tile
             unsigned sb = 0, vbuf = 0, p_phase = 0;                  // the buffers that scores go to and p comes from, p's phase
@@ -526,7 +515,6 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
             unsigned walked = 0;
             auto there = [&]() {
                 if (ok) ok = warp_wait(kv_full + 8 * slot, phase, &quit, a, 205);
-                if (MODE == COPIED) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // ordinary copies before the products' reads
             };
             auto onward = [&]() {
                 ++walked;
@@ -546,14 +534,14 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                 onward();
             };
             // What lies behind the last position that the block sees, and what has no page, must be zero in V: its p is 0, and 0 times what happens
-            // to lie there need not be.  (Where the halves share the tile both do it; copies of 16 bytes bring the zeros.)
+            // to lie there need not be.  (Where the halves share the tile both do it.)
             auto clean = [&](uint32_t v, int valid, unsigned groups) {
                 for (int i = lane; i < KEYS * 8; i += 32) {
                     const int row = i >> 3;
                     if (row < valid && (groups >> (row >> 4) & 1)) continue;
 #pragma unroll
                     for (int b = 0; b < L::BANDS; ++b)
-                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(v + b * BAND + i * 16), "r"(0) : "memory");
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(v + (row >> 3) * GROUP + b * NEXT_BAND + (i & 63) * 16), "r"(0) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -574,7 +562,7 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                     const uint32_t bar = my_s + 8 * sb;
                     if (lane == 0) bar_arrive(bar);                  // hands on what the copies' warp noted of the tile
                     fence_after();
-                    mma_scores<HD>(s_col + sb * SUB, q_desc, desc_of(k) + (u & 1) * SUB_STEP, S_DESC, bar);
+                    mma_scores<HD, PAGED>(s_col + sb * SUB, q_desc, desc_of(k, NEXT_BAND) + (u & 1) * SUB_STEP, S_DESC, bar);
                     sb ^= 1;
                     if (u + 1 == n) commit(my_q_empty);
                     if ((u & 1) || u + 1 == n) commit(k_bar);
@@ -590,13 +578,13 @@ __global__ void __launch_bounds__(threads_of(MODE == COPIED), 1) tensor_kernel(c
                             if (own) pass(h ? (t == T - 1 ? 1 : 2) : (t == 0 ? 1 : 2));
                             take(v, v_bar);
                             const int valid = it.kv - (job.j0 + t) * KEYS;
-                            const unsigned groups = MODE == TILED ? info[(step0 + t) % INFO] : 0xffu;
-                            if (MODE != COPIED && ok && (valid < KEYS || groups != 0xffu)) clean(v, valid, groups);
+                            const unsigned groups = PAGED ? info[(step0 + t) % INFO] : 0xffu;
+                            if (ok && (valid < KEYS || groups != 0xffu)) clean(v, valid, groups);
                         }
                         if (ok) ok = warp_wait(my_p + 8 * vbuf, p_phase, &quit, a, 206);
                         if (!ok) break;
                         fence_after();
-                        mma_values(o_col, s_col + vbuf * SUB, desc_of(v) + (u & 1) * SUB_STEP, O_DESC, u > 0, my_o + 8 * vbuf);
+                        mma_values<HD, PAGED>(o_col, s_col + vbuf * SUB, desc_of(v, NEXT_BAND) + (u & 1) * SUB_STEP, O_DESC, u > 0, my_o + 8 * vbuf);
                         p_phase ^= vbuf;
                         vbuf ^= 1;
                         if ((u & 1) || u + 1 == n) commit(v_bar);

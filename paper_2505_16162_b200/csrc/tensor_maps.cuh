@@ -25,7 +25,7 @@ inline EncodeTiledFn encode_tiled_fn() {
 // places outside read as zero.
 inline bool bf16_map(CUtensorMap *m, const void *base, int dims, const cuuint64_t *sizes, const cuuint64_t *strides, const cuuint32_t *box) {
     const EncodeTiledFn fn = encode_tiled_fn();
-    const cuuint32_t one[3] = {1u, 1u, 1u};
+    const cuuint32_t one[4] = {1u, 1u, 1u, 1u};
     return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)dims, const_cast<void *>(base), sizes, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
