@@ -26,13 +26,13 @@ namespace cg = cooperative_groups;
 
 constexpr int ACC_NT = 256, ACC_NW = ACC_NT / 32;
 constexpr int ACC_ROWS = 1024;            // rows of a request that are looked at
-// Blocks of a request: as many as find room at once, and a thousand ids at least for each, below that a meeting of more blocks costs what they save.  1 / 2 / 4 / 8 / 16 of
-// them, drafts drawn: 24 requests of 25 rows and 1000 ids 7.6 / 10 / 10 / 10 / 16 us, of 32000 24 / 17 / 13 / 12 / 13, of 152064 86 / 49 / 31 / 22 / 17; 400 requests of 9 rows and
-// 32000 ids 41 / 39 / 47 / 68 / 127.  With more than 4096 ids a block they pay up to three and a half a processor (32 requests of 152064 ids as 16 blocks 21 us, as 8 28), else
-// up to two.
-inline int blocks_of(int requests, int vocab, int processors) {
+// Blocks of a request: as many as find room at once, and a thousand ids at least for each, below that a meeting of more blocks costs what they save.  1 / 8 / 16 of them: 24 requests
+// of 25 rows and 32000 ids 25 / 12 / 14 us where drafts are drawn, 16 / 11 / 14 where they are chosen; of 152064 ids 86 / 23 / 17 and 37 / 14 / 15; 400 requests of 9 rows and 32000
+// ids 39 / 66 / 130 and 23 / 55 / 117.  Where a block has more than 10 000 values to read they pay up to three and a half a processor (32 requests of 152064 ids, drawn, as 16
+// blocks 22 us, as 8 28), else up to two.
+inline int blocks_of(int requests, int vocab, bool drawn, int processors) {
     for (int c = 16; c > 1; c /= 2)
-        if (2ll * requests * c <= (vocab > 4096 * c ? 7 : 4) * processors && vocab >= 1000 * c) return c;
+        if (2ll * requests * c <= (vocab * (drawn ? 2ll : 1ll) > 10000 * c ? 7 : 4) * processors && vocab >= 1000 * c) return c;
     return 1;
 }
 
@@ -86,54 +86,81 @@ template <int C> __device__ __forceinline__ int child_token(const AcceptShared<C
 // A lane's share of a sum over ids [i0, i1), N values of a row on their way.  Pieces of code of their own: a round calls them from several places, and a block that comes to an
 // instruction for the first time waits for it (unrolled in place, 32 values at a time and the draw's running sums with them: one row of 152064 ids 19 us for 7).
 // A float's bits, moved to where a double has its own, are its value times 2^-896, zeros and subnormals included; the sum is scaled back.  Two integer operations, where a
-// conversion takes 11 clocks a warp (a row of 152064 ids by one block: 32 us so, 24 with the bits).  What is not a finite number, or has a sign, is done by conversions.
+// conversion takes 11 clocks a warp (a row of 152064 ids by one block: 32 us so, 24 with the bits).  What is not a finite number, or has a sign, comes to 2^-768 and more (no other
+// float does, its sign or its exponent's bits see to it): then the sum is formed once more by conversions.
 constexpr int OUTS = 4;                   // ids that a sum of values can leave out
-constexpr double SCALED_BACK = 0x1p896;
+constexpr double SCALED_BACK = 0x1p896, TOO_LARGE = 0x1p-768;
 __device__ __forceinline__ double scaled(unsigned bits) { return __hiloint2double(bits >> 3, bits << 29); }
-static __device__ __noinline__ double sum_values(const float *p, int i0, int i1, int out0, int out1, int out2, int out3) {
-    constexpr int N = 8;
-    double s[2] = {0.0, 0.0};
-    unsigned top = 0;
-    auto in = [&](int id) { return id < i1 && id != out0 && id != out1 && id != out2 && id != out3; };
-    i0 += threadIdx.x & 31;
-#pragma unroll 1
-    for (int i = i0; i < i1; i += 32 * N) {
-        unsigned v[N];
+// Four ids from `id` on, those below `end`; zeros behind.
+__device__ __forceinline__ void four(const float *p, int id, int end, bool aligned, unsigned (&v)[4]) {
+    if (aligned && id + 4 <= end) {
+        const uint4 w = __ldg(reinterpret_cast<const uint4 *>(p + id));
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+    } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = in(i + 32 * e) ? __float_as_uint(p[i + 32 * e]) : 0u;
-#pragma unroll
-        for (int e = 0; e < N; ++e) { s[e & 1] += scaled(v[e]); top = max(top, v[e]); }
+        for (int j = 0; j < 4; ++j) v[j] = id + j < end ? __float_as_uint(__ldg(p + id + j)) : 0u;
     }
-    if (top < 0x7f800000u) return (s[0] + s[1]) * SCALED_BACK;
+}
+static __device__ __noinline__ double sum_values(const float *p, int i0, int i1, int out0, int out1, int out2, int out3) {
+    constexpr int N = 4;
+    double s[2] = {0.0, 0.0};
+    const bool aligned = (reinterpret_cast<uintptr_t>(p + i0) & 15u) == 0, outs = out0 < i1;
+    const int first = i0 + 4 * (threadIdx.x & 31);
+#pragma unroll 1
+    for (int i = first; i < i1; i += 128 * N) {
+        unsigned v[N][4];
+#pragma unroll
+        for (int e = 0; e < N; ++e) four(p, i + 128 * e, i1, aligned, v[e]);
+        if (outs) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const unsigned d0 = out0 - i - 128 * e, d1 = out1 - i - 128 * e, d2 = out2 - i - 128 * e, d3 = out3 - i - 128 * e;
+                if (min(min(d0, d1), min(d2, d3)) < 4u)
+#pragma unroll
+                    for (unsigned j = 0; j < 4; ++j)
+                        if (j == d0 || j == d1 || j == d2 || j == d3) v[e][j] = 0u;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j & 1] += scaled(v[e][j]);
+    }
+    if (s[0] + s[1] < TOO_LARGE) return (s[0] + s[1]) * SCALED_BACK;
     double t = 0.0;
 #pragma unroll 1
-    for (int i = i0; i < i1; i += 32) t += in(i) ? (double)p[i] : 0.0;
+    for (int i = first; i < i1; i += 128)
+        for (int j = i; j < min(i + 4, i1); ++j) t += j == out0 || j == out1 || j == out2 || j == out3 ? 0.0 : (double)p[j];
     return t;
 }
 static __device__ __noinline__ double sum_left(const float *p, const float *q, double a, double b, int i0, int i1) {
-    constexpr int N = 8;
+    constexpr int N = 2;
     double s[2] = {0.0, 0.0};
     unsigned top = 0;
-    i0 += threadIdx.x & 31;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(p + i0) | reinterpret_cast<uintptr_t>(q + i0)) & 15u) == 0;
+    const int first = i0 + 4 * (threadIdx.x & 31);
 #pragma unroll 1
-    for (int i = i0; i < i1; i += 32 * N) {
-        unsigned v[N], u[N];
+    for (int i = first; i < i1; i += 128 * N) {
+        unsigned v[N][4], u[N][4];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            v[e] = i + 32 * e < i1 ? __float_as_uint(p[i + 32 * e]) : 0u;
-            u[e] = i + 32 * e < i1 ? __float_as_uint(q[i + 32 * e]) : 0u;
+            four(p, i + 128 * e, i1, aligned, v[e]);
+            four(q, i + 128 * e, i1, aligned, u[e]);
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const double x = fma(a, scaled(v[e]), -b * scaled(u[e]));
-            s[e & 1] += __double2hiint(x) < 0 ? 0.0 : x;
-            top = max(top, max(v[e], u[e]));
-        }
+        for (int e = 0; e < N; ++e)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const double x = fma(a, scaled(v[e][j]), -b * scaled(u[e][j]));
+                s[j & 1] += __double2hiint(x) < 0 ? 0.0 : x;
+                top = max(top, u[e][j]);
+            }
     }
-    if (top < 0x7f800000u) return (s[0] + s[1]) * SCALED_BACK;
+    if (top < 0x7f800000u && s[0] + s[1] < a * TOO_LARGE) return (s[0] + s[1]) * SCALED_BACK;
     double t = 0.0;
 #pragma unroll 1
-    for (int i = i0; i < i1; i += 32) t += left_of(a, b, p[i], q[i]);
+    for (int i = first; i < i1; i += 128)
+        for (int j = i; j < min(i + 4, i1); ++j) t += left_of(a, b, p[j], q[j]);
     return t;
 }
 // Whether an id is the token of a child, for the 32 ids from `base` on.
@@ -297,6 +324,10 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
     int row0, n_all;
     rows_of(a.row_start, a.R, b, row0, n_all);
     const int n = min(n_all, ACC_ROWS);
+    const int S = ((V + C - 1) / C + 31) & ~31;                      // ids of a block
+    auto first_id = [&](int r) { return (int)min((long long)V, (long long)r * S); };
+    const int lo = first_id(rank), hi = first_id(rank + 1);
+    Weights w{a.p + (size_t)row0 * V, a.q ? a.q + (size_t)row0 * V : nullptr, ALL, 0, n, 1.0, 0.0};
     const float u_final = a.u_final[b];
     for (int i = tid; i < n; i += ACC_NT) {
         const int up = a.parent[row0 + i], x = a.token[row0 + i];
@@ -319,11 +350,7 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
         __syncthreads();
     }
     if (C > 1) cluster.barrier_wait();
-    const int S = ((V + C - 1) / C + 31) & ~31;                      // ids of a block
-    auto first_id = [&](int r) { return (int)min((long long)V, (long long)r * S); };
-    const int lo = first_id(rank), hi = first_id(rank + 1);
     int kept = 0, turn = 0;
-    Weights w{a.p + (size_t)row0 * V, a.q ? a.q + (size_t)row0 * V : nullptr, ALL, 0, n, 1.0, 0.0};
     double z = 1.0, total = -1.0;                                    // total: the sum that the last pass over the weights as they are gave; -1: there was none
     int last = 0;
     auto step_to = [&](int c) {

@@ -54,7 +54,7 @@ knnssd_status knnssd_tree_accept(const float *p_dev, const float *q_dev_or_null,
     if (vocab > KNNSSD_MAX_VOCAB || n_requests > KNNSSD_MAX_REQUESTS) return KNNSSD_ERR_CAPACITY;
     const trees::AcceptArgs a{p_dev, q_dev_or_null, vocab, row_token_dev, row_parent_dev, row_start_dev, n_requests, n_rows, u_accept_dev, u_final_dev, path_dev, n_accepted_dev, next_token_dev};
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-    switch (trees::blocks_of(n_requests, vocab, sm_count())) {
+    switch (trees::blocks_of(n_requests, vocab, q_dev_or_null != nullptr, sm_count())) {
     case 16: return launch_accept<16>(a, s);
     case 8: return launch_accept<8>(a, s);
     case 4: return launch_accept<4>(a, s);

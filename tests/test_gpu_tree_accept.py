@@ -342,3 +342,23 @@ def test_refusals_of_the_binding(kb):
         thin = [p[..., :32].contiguous() for p in pools]
         kb.knnssd_keep_rows(kb.PagePools(thin[:1], thin[1:]), table, lens, start, path)
     assert e.value.status == 2
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("V", [999, 1002, 8193])
+def test_rows_that_begin_anywhere(kb, drawn, V):
+    """p and q whose rows, and whose own beginnings, are not on 16-byte boundaries."""
+    rng = np.random.default_rng(V)
+    for shift in (0, 1, 3):
+        r = Round(V + shift, [_parents(rng, 9, 3) for _ in range(5)], V, drawn)
+        p, q, *rest = r.on_device()
+        moved = []
+        for x in (p, q):
+            if x is not None:
+                wide = torch.full((x.numel() + 8,), torch.nan, device="cuda")
+                wide[shift:shift + x.numel()] = x.flatten()
+                x = wide[shift:shift + x.numel()].view(x.shape)
+            moved.append(x)
+        out = [torch.full((n,), 77, **I32) for n in (len(r.token), 5, 5)]
+        kb.knnssd_tree_accept(*moved, *rest, *out)
+        assert tuple(t.tolist() for t in out) == r.want()
