@@ -4,9 +4,9 @@
 #include "../../include/knnssd.h"
 #include "host_common.cuh"
 #include "row_attention.cuh"
-#include "short_attention.cuh"
 #include "tensor_attention.cuh"
 #include "tensor_maps.cuh"
+#include "tree_rows.cuh"
 
 #include <algorithm>
 #include <atomic>
@@ -121,25 +121,48 @@ template <int HD, bool PAGED, bool TREE = false> knnssd_status launch_tensor(att
     return launched();
 }
 
-// Trees over short contexts: whether one block for 16 rows and all positions that the table has room for is the sooner way, by microseconds that were measured.  A block takes 3 and,
-// for 128 positions of 128 dimensions, 0.8 (bf16), 1.45 (fp32 rows, bf16 cache) or 3.6 (fp32; contexts filled two thirds of their tables), one block a processor at a time; the ways that
-// share positions out take 16 or 20 whatever the sizes and then read some 7 GB/ms, half of it where the cache is fp32.  One request of 12 rows, 32 heads and 300 positions
-// 9.7 us for 21; 8 requests 18 for 34; of 700 positions and 40 rows 64 for 46; 4 fp32 heads of 64, one request of 60 positions 5.4 for 16.
-inline bool is_short(attn::Args a, int dtype, int cache_dtype, int hd) {
-    share_heads(a, shortattn::ROWS);
+// Trees over short contexts: whether a block for 16 rows and all positions that the table has room for is the sooner way, and with how many warps (0: it is not), by microseconds that were
+// measured.  A block of eight warps, one a processor at a time, takes 3 and, for 128 positions of 128 dimensions, 0.8 (bf16), 1.45 (fp32 rows, bf16 pages) or 2.4 (fp32; contexts that
+// fill two thirds of their tables); of four warps, two a processor, 3.5 and 2.2 times that.  The ways that share positions out take 16 to 25 whatever the sizes and then some 7 GB of
+// bf16 pages a millisecond, half of that of fp32 ones.  8 / 4 warps / shared out: one request of 48 rows, 32 bf16 heads and 300 positions 10 / 14 / 24 us, 8 requests of 12 rows 18 / 14 / 34;
+// 32 requests of 60 positions 36 / - / 30.
+inline int short_warps(attn::Args a, int dtype, int cache_dtype, int hd) {
+    share_heads(a, treerows::ROWS);
     const long long positions = (long long)a.max_pages << a.page_shift, tiles = (long long)a.R / a.tb + a.B;
-    if (tiles > 65535 || positions > 4096) return false;
-    const double step = hd / 128.0 * (cache_dtype == 0 ? 3.6 : dtype == 0 ? 1.45 : 0.8), ctas = sm_count();
-    const double own = 3.0 + std::ceil(tiles * a.nvh / ctas) * (3.0 + step * positions / 128.0);
-    const double shared = (dtype == 0 && hd == 64 ? 16.0 : 20.0) + (double)a.B * a.KV * positions * hd * (cache_dtype == 0 ? 16.0 : 4.0) / 7e6;
-    return own < shared;
+    if (tiles > 65535 || positions > 4096) return 0;
+    const double step = hd / 128.0 * (cache_dtype == 0 ? 2.4 : dtype == 0 ? 1.45 : 0.8) * positions / 128.0, blocks = (double)tiles * a.nvh / sm_count();
+    const double eight = 3.0 + std::ceil(blocks) * (3.0 + step), four = 3.0 + std::max(1.0, blocks / 2) * (3.5 + 2.2 * step);
+    const double shared = (dtype == 0 && hd == 64 ? 16.0 : cache_dtype == 0 ? 25.0 : 20.0) + (double)a.B * a.KV * positions * hd * (cache_dtype == 0 ? 16.0 : 4.0) / 7e6;
+    if (std::min(eight, four) >= shared) return 0;
+    return eight <= four || cache_dtype == 0 ? 8 : 4;
 }
-template <int HD, typename QT, typename KT> knnssd_status launch_short(attn::Args a, cudaStream_t s) {
+template <int HD, typename QT, typename KT, int W> knnssd_status launch_short_of(attn::Args a, cudaStream_t s) {
+    using L = treerows::Lay<HD, QT, KT, W>;
     static bool configured[kMaxDevices] = {};
-    const auto kernel = shortattn::short_kernel<HD, QT, KT>;
-    if (!allow_smem(kernel, shortattn::smem_bytes<HD>(), configured)) return KNNSSD_ERR_CUDA;
-    share_heads(a, shortattn::ROWS);
-    launch_chained(kernel, dim3(a.nvh, a.R / a.tb + a.B), dim3(shortattn::NT), shortattn::smem_bytes<HD>(), s, a);
+    const auto kernel = treerows::tree_rows_kernel<HD, QT, KT, W>;
+    if (!allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
+    share_heads(a, treerows::ROWS);
+    launch_chained(kernel, dim3(a.nvh, a.R / a.tb + a.B), dim3(L::NT), L::SMEM, s, a);
+    return launched();
+}
+template <int HD> knnssd_status launch_short(const attn::Args &a, int dtype, int cache_dtype, int warps, cudaStream_t s) {
+    if (cache_dtype == 0) return launch_short_of<HD, float, float, 8>(a, s);
+    if (dtype == 0) return warps == 8 ? launch_short_of<HD, float, bf16_t, 8>(a, s) : launch_short_of<HD, float, bf16_t, 4>(a, s);
+    return warps == 8 ? launch_short_of<HD, bf16_t, bf16_t, 8>(a, s) : launch_short_of<HD, bf16_t, bf16_t, 4>(a, s);
+}
+template <int HD> knnssd_status launch_tree_rows(attn::Args a, cudaStream_t s) {
+    using L = treerows::Lay<HD, float, float, 0>;
+    static bool configured[kMaxDevices] = {};
+    const auto kernel = treerows::tree_rows_kernel<HD, float, float, 0>;
+    if (!allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
+    share_heads(a, treerows::ROWS);
+    a.extra = 128;
+    a.least_run = 256;
+    a.most = (int)std::min((long long)L::BLOCKS * sm_count(), 128ll * a.nvh * std::max(a.B, a.R / a.tb));
+    Scratch mem(s);
+    if (!get_parts(mem, a, a.most, treerows::ROWS, HD)) return KNNSSD_ERR_CUDA;
+    launch_chained(kernel, dim3(a.most), dim3(L::NT), L::SMEM, s, a);
+    launch_chained(attn::merge_kernel<HD, float, false, treerows::ROWS>, dim3(a.most - 1, (a.tb * a.gs + 7) / 8), dim3(256), 0, s, a);
     return launched();
 }
 
@@ -184,19 +207,18 @@ knnssd_status paged_attention(const void *q_dev, int dtype, int n_rows, long lon
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     try {
         if constexpr (TREE)
-            if (is_short(a, dtype, cache_dtype, head_dim)) {
-                if (dtype == 1) return head_dim == 128 ? launch_short<128, bf16_t, bf16_t>(a, s) : launch_short<64, bf16_t, bf16_t>(a, s);
-                if (head_dim == 128) return cache_dtype == 0 ? launch_short<128, float, float>(a, s) : launch_short<128, float, bf16_t>(a, s);
-                return cache_dtype == 0 ? launch_short<64, float, float>(a, s) : launch_short<64, float, bf16_t>(a, s);
-            }
+            if (const int warps = short_warps(a, dtype, cache_dtype, head_dim))
+                return head_dim == 128 ? launch_short<128>(a, dtype, cache_dtype, warps, s) : launch_short<64>(a, dtype, cache_dtype, warps, s);
         if (dtype == 1) {
             const int most_rows = max_fresh > 0 ? std::min(max_fresh, a.R) : a.R;
             // a coordinate of the copies, eight rows, has 31 bits
             if ((long long)n_pages * n_kv_heads > INT_MAX / (page_size / 8)) return KNNSSD_ERR_CAPACITY;
             return head_dim == 128 ? launch_tensor<128, true, TREE>(a, most_rows, s) : launch_tensor<64, true, TREE>(a, most_rows, s);
         }
-        if (head_dim == 128) return cache_dtype == 0 ? launch_rows<128, float, true, TREE>(a, s) : launch_rows<128, bf16_t, true, TREE>(a, s);
-        return cache_dtype == 0 ? launch_rows<64, float, true, TREE>(a, s) : launch_rows<64, bf16_t, true, TREE>(a, s);
+        if constexpr (TREE)
+            if (cache_dtype == 0) return head_dim == 128 ? launch_tree_rows<128>(a, s) : launch_tree_rows<64>(a, s);
+        if (head_dim == 128) return cache_dtype == 0 ? launch_rows<128, float, true>(a, s) : launch_rows<128, bf16_t, true, TREE>(a, s);
+        return cache_dtype == 0 ? launch_rows<64, float, true>(a, s) : launch_rows<64, bf16_t, true, TREE>(a, s);
     } catch (...) { return KNNSSD_ERR_CUDA; }
 }
 

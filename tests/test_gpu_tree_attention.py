@@ -153,12 +153,12 @@ def test_words_of_all_kinds(kb, dtype, cache, H, KV, hd, page, more):
 @pytest.mark.parametrize("dtype,cache", KINDS)
 @pytest.mark.parametrize("lens,fresh", [([300, 0, 77], [5, 64, 200]), ([20011], [1]), ([40] * 300, [3] * 300)])
 def test_chains_are_the_rows_of_paged_attention(kb, dtype, cache, lens, fresh):
-    """To the bit where the table has room for long contexts; short ones have a kernel of their own."""
+    """To the bit for bf16 rows where the table has room for long contexts, which is the same kernel."""
     for wide in (300, 2):
         p = Trees(kb, 9, lens, [list(range(-1, n - 1)) for n in fresh], 2, 128, 16, cache, wide=wide)
         q = p.q(6, 128, dtype)
         got = p.run(kb, q)
-        assert wide == 2 or torch.equal(got, Paged.run(p, kb, q))
+        assert wide == 2 or dtype == "fp32" or torch.equal(got, Paged.run(p, kb, q))
         _check(got, *p.want(q))
 
 
