@@ -9,7 +9,7 @@
 // 13 rows, 4 fp32 heads of 64 over 96 positions 5.7 us, where the ways for long contexts take 17; one request of 12 rows, 32 bf16 heads over 300 positions 9.7 for 21.
 //
 // Else a block has an equal run of all items' positions, as in attention_items.cuh, and parts of items are put together by the merge.  fp32 pages: the rows kernel has room for one warp a
-// scheduler beside their copies, here there are two: 8 requests of 25 rows, 40 heads over 1280 positions 191 us for 288 (2.2 TB/s; the terms of K and V and six products of each,
+// scheduler beside their copies, here there are two: 8 requests of 25 rows, 40 heads over 1280 positions 174 us for 288 (2.5 TB/s; the terms of K and V and six products of each,
 // 16 rows at a time), one of 8000 positions 81 for 117.  (bf16 pages stay with the rows kernel, whose copies run ahead: 94 us for 109.)
 #pragma once
 
