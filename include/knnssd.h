@@ -559,7 +559,7 @@ knnssd_status knnssd_tree_agree(const int *row_best_dev, const int *row_token_de
 /*
  * K and V of the kept rows together: in each of n_pools pools (all layers' K and V) and for j = 0, 1, .. what lies at position lens[b] + path[row_start[b] + j] goes to
  * lens[b] + j, as long as path ascends and stays below the request's rows.  Positions without a page are left out.
- *   pools_host  HOST [n_pools] of DEVICE pointers, read during the call: pools of one type and size, as k_pages_dev above; cache_dtype, n_kv_heads, head_dim, page_size,
+ *   pools_host  HOST [n_pools] of DEVICE pointers, read during the call: pools of one type and size, no two the same, as k_pages_dev above; cache_dtype, n_kv_heads, head_dim, page_size,
  *               n_pages, max_pages and the limits on them as there
  */
 knnssd_status knnssd_keep_rows(void *const *pools_host, int n_pools, int cache_dtype, int n_kv_heads, int head_dim, int page_size,

@@ -511,6 +511,8 @@ class PagePools:
         self.cache = _type(self._keep[0], "k_pages")
         for t in self._keep:                                         # all as the first one
             self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = _pages(self._keep[0], t, self.device)
+        if len({t.data_ptr() for t in self._keep}) != len(self._keep):
+            raise ValueError("a pool is given twice")
         self.pointers = (C.c_void_p * len(self._keep))(*[t.data_ptr() for t in self._keep])
 
 

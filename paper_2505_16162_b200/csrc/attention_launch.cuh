@@ -129,8 +129,9 @@ template <int HD, bool PAGED, bool TREE = false> knnssd_status launch_tensor(att
 inline int short_warps(attn::Args a, int dtype, int cache_dtype, int hd) {
     share_heads(a, treerows::ROWS);
     const long long positions = (long long)a.max_pages << a.page_shift, tiles = (long long)a.R / a.tb + a.B;
-    if (tiles > 65535 || positions > 4096) return 0;
-    const double step = hd / 128.0 * (cache_dtype == 0 ? 2.4 : dtype == 0 ? 1.45 : 0.8) * positions / 128.0, blocks = (double)tiles * a.nvh / sm_count();
+    const double blocks = (double)tiles * a.nvh / sm_count();
+    if (blocks > 8.0 || positions > 2048) return 0;                  // beyond what the figures are of
+    const double step = hd / 128.0 * (cache_dtype == 0 ? 2.4 : dtype == 0 ? 1.45 : 0.8) * positions / 128.0;
     const double eight = 3.0 + std::ceil(blocks) * (3.0 + step), four = 3.0 + std::max(1.0, blocks / 2) * (3.5 + 2.2 * step);
     const double shared = (dtype == 0 && hd == 64 ? 16.0 : cache_dtype == 0 ? 25.0 : 20.0) + (double)a.B * a.KV * positions * hd * (cache_dtype == 0 ? 16.0 : 4.0) / 7e6;
     if (std::min(eight, four) >= shared) return 0;

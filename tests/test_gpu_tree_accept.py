@@ -320,7 +320,7 @@ def test_pools_beyond_32_bits(kb):
 
 def test_refusals_of_the_binding(kb):
     pools, table = _pools(3, 2, [10], [4], 2, 64, 16, torch.bfloat16)
-    for k, v in (([], []), ([pools[0]], []), ([pools[0]], [pools[1].float()]), ([pools[0]], [pools[1][:1]]), ([pools[0].cpu()], [pools[1].cpu()]), ([pools[0].half()], [pools[1].half()])):
+    for k, v in (([], []), ([pools[0]], []), ([pools[0]], [pools[1].float()]), ([pools[0]], [pools[1][:1]]), ([pools[0].cpu()], [pools[1].cpu()]), ([pools[0].half()], [pools[1].half()]), ([pools[0]], [pools[0]])):
         with pytest.raises(ValueError):
             kb.PagePools(k, v)
     ok = kb.PagePools([pools[0]], [pools[1]])

@@ -172,6 +172,18 @@ def test_long_contexts_in_many_parts(kb, dtype, cache, H, KV, hd, lens, rows):
 
 
 @pytest.mark.parametrize("dtype,cache", KINDS)
+@pytest.mark.parametrize("H,KV,n,most", [(2, 1, 300, 40), (8, 1, 700, 90), (3, 1, 1000, 20)])
+def test_more_requests_than_a_block_has_threads(kb, dtype, cache, H, KV, n, most):
+    rng = np.random.default_rng(n)
+    p = Trees(kb, n, rng.integers(0, most, n).tolist(), [_parents(rng, int(r), 2) for r in rng.integers(0, 3, n)], KV, 64, 16, cache)
+    q = p.q(H, 64, dtype)
+    want, tol = p.want(q)
+    for table in (p.table, _wider(p.table, 300)):
+        p.table = table
+        _check(p.run(kb, q), want, tol)
+
+
+@pytest.mark.parametrize("dtype,cache", KINDS)
 def test_many_requests_of_all_lengths(kb, dtype, cache):
     rng = np.random.default_rng(5)
     n = 400
