@@ -41,7 +41,7 @@ class TreeBatch(mr.Batch):
         super().__init__(shape, weights, n_requests, max_seq, n_pages, mask)
         self.widths, self.temperature, self.top_p = list(widths), temperature, top_p
         self.parents, self.levels = tree_of(widths)
-        self.pools2 = kb.PagePools([k for k, _ in self.pools], [v for _, v in self.pools])
+        self.page_pools = kb.PagePools([k for k, _ in self.pools], [v for _, v in self.pools])
         self.g = torch.Generator(device="cuda").manual_seed(seed)
 
     def attend(self, q, k_pages, v_pages, s):
@@ -92,7 +92,7 @@ class TreeBatch(mr.Batch):
         else:
             u, last = torch.rand(n * L, generator=self.g, device="cuda"), torch.rand(self.B, generator=self.g, device="cuda")
             kb.knnssd_tree_accept(self.probabilities(logits), q.flatten(0, 1), flat, parent, s["start"], u, last, path, accepted, nxt)
-        kb.knnssd_keep_rows(self.pools2, self.table, self.lens, s["start"], path)
+        kb.knnssd_keep_rows(self.page_pools, self.table, self.lens, s["start"], path)
         self.lens = self.lens + torch.where(fresh > 0, accepted + 1, 0).int()
         out = [[] for _ in range(self.B)]
         for b, row, p, m in zip(where.tolist(), tokens.tolist(), path.view(L, n).tolist(), nxt[where].tolist()):
