@@ -533,8 +533,9 @@ knnssd_status knnssd_tree_attention(const void *q_dev, int dtype, int n_rows, lo
  * they were chosen (by rank, say).  From row 0 on, the children of the row kept last are tested in row order.  With w what is left of its p, Z the sum of w (1 at first):
  *   q given:  child c is kept iff u_accept[c] Z q(x_c) < w(x_c); else w becomes max(0, w / Z - q)
  *   no q:     child c is kept iff u_accept[c] Z < w(x_c);        else w(x_c) becomes 0
- * Behind the last row kept the token is the smallest x with w_0 + .. + w_x > u_final sum(w), drawn from p where nothing is left of it (-1 if p has no weight at all, or a
- * NaN).  Tests and sums in 64 bits.  The tokens have p's distribution whatever was drafted.
+ * Behind the last row kept the token is the smallest x with w_0 + .. + w_x > u_final sum(w), drawn from p where nothing is left of it.  It is -1 where that row of p has no
+ * weight at all, a NaN or +inf, and where a draft behind the row was rejected and its row of q has a NaN (no draft behind that one is kept then: a row is summed up for the
+ * first time when one of its drafts is rejected).  Tests and sums in 64 bits.  The tokens have p's distribution whatever was drafted.
  *   row_token_dev [n_rows], row_parent_dev [n_rows]  in; a row whose token is outside [0, vocab), or whose parent is not a row before it, is passed over with all that follow it
  *   u_accept_dev [n_rows], u_final_dev [n_requests]  uniforms in [0, 1) (u_final outside: token -1); those of rows 0 are not used
  *   path_dev [n_rows]         out: path[row_start[b] + j] the j-th row kept, within its request, row 0 first; -1 behind the last one and for rows that no request has

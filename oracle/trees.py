@@ -6,7 +6,8 @@ token, row i > 0 follows row parent[i] < i.  Siblings are tested in row order.
 * ``ancestors`` / ``words``: which rows a row sees, and the same as 64 bits counted back from its own slot;
 * ``accept``: speculative sampling with several drafts behind a row.  Drafts that were drawn from q are kept with probability min(1, w(x) / (Z q(x)))
   where w is what the rejections so far have left of p and Z its sum; a rejection leaves max(0, w / Z - q).  Drafts that were chosen (no q) are kept with
-  probability w(x) / Z; a rejection leaves w without x.  The token behind the last row kept is drawn from what is left, from p where that is nothing;
+  probability w(x) / Z; a rejection leaves w without x.  The token behind the last row kept is drawn from what is left, from p where that is nothing.
+  Where p's row, or what a rejection leaves of it, is not finite, no further draft is kept and there is no token;
 * ``agree``: the greedy form.
 
 Pinned in ``tests/test_oracle_trees.py``: the emitted distribution is p, chains agree with ``oracle.sampling``, words against ``ancestors``.
@@ -77,10 +78,14 @@ def accept(p, q, token, parent, u_accept, u_final):
                 w[x] = 0.0
             elif z > 0:
                 w = np.maximum(w / z - q[node], 0.0)
-            z = math.fsum(w)
+            z = math.fsum(w) if np.isfinite(p[node]).all() and np.isfinite(w).all() else math.nan
+            if math.isnan(z):
+                break
         if go is None:
             break
         kept.append(go)
+    if math.isnan(z) or not np.isfinite(p[kept[-1]]).all():
+        return kept, -1
     if not w.any():
         w = p[kept[-1]]
     return kept, (_draw(w, float(u_final)) if w.any() else -1)

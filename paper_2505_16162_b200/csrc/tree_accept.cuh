@@ -5,7 +5,7 @@
 //   drafts drawn from q[node], each by itself:  child c is kept iff u_c Z q[node](x_c) < w(x_c); else w <- max(0, w / Z - q[node]), Z <- sum w
 //   drafts chosen, not drawn (no q):            child c is kept iff u_c Z < w(x_c);              else w(x_c) <- 0, Z <- sum w
 // A kept child is the next node.  Where none is left the token after it is the smallest x with w_0 + .. + w_x > u_final sum(w), from p[node] if nothing is left of it.
-// Either way the tokens are distributed as p has them.  Random numbers are inputs.
+// Either way the tokens are distributed as p has them.  Random numbers are inputs.  A sum that is NaN keeps no further child and ends in no token.
 //
 // A request is the work of a cluster of C blocks, each with a contiguous part of the ids.  All blocks take the same decisions from the same numbers: the tests need one value
 // of p and of q a draft, fetched for all drafts at once at the start.  Only a rejection reads a row: a pass over the ids, a sum per warp, a meeting of the cluster.  The last pass's sums
@@ -80,7 +80,10 @@ __device__ __forceinline__ int next_child(const int *parent, int n, int node, in
 // y / Z - q have the same positive part); its values without those of the children of `node`.
 enum { ALL = 0, DRAWN = 1, CHOSEN = 2 };
 struct Weights { const float *p, *q; int kind, node, n; double a, b; };
-__device__ __forceinline__ double left_of(double a, double b, float p, float q) { return fmax(fma(a, (double)p, -b * (double)q), 0.0); }
+__device__ __forceinline__ double left_of(double a, double b, float p, float q) {
+    const double x = fma(a, (double)p, -b * (double)q);
+    return x < 0.0 ? 0.0 : x;                                        // NaN stays
+}
 template <int C> __device__ __forceinline__ int child_token(const AcceptShared<C> &sh, const Weights &w, int i) { return i < w.n && sh.parent[i] == w.node ? sh.token[i] : -1; }
 
 // A lane's share of a sum over ids [i0, i1), N values of a row on their way.  Pieces of code of their own: a round calls them from several places, and a block that comes to an
@@ -283,6 +286,12 @@ template <int C> __device__ __forceinline__ int find_id(AcceptShared<C> &sh, con
     return past ? base + __ffs(past) - 1 : some ? base + 31 - __clz(some) : base;
 }
 
+// Whether p at the token of one of the node's children is not finite: the sum without the children does not show it.  The same in every warp.
+template <int C> __device__ __forceinline__ bool odd_child(const AcceptShared<C> &sh, const Weights &w) {
+    bool odd = false;
+    for (int i = threadIdx.x & 31; i < w.n; i += 32) odd |= sh.parent[i] == w.node && !isfinite(sh.p_of[i]);
+    return __any_sync(0xffffffffu, odd);
+}
 // Drafts chosen: of the children of w.node behind row c, which was rejected, the first that is kept; `rest`: the sum without all of the node's children.  n: none is.
 // The sum that a child is held against is the rest and the children from it on: all are tested at once.  The same in every warp.
 template <int C> __device__ __forceinline__ int first_kept(const AcceptShared<C> &sh, const Weights &w, int c, double rest) {
@@ -379,13 +388,14 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
             w.b = w.b / z + 1.0;
         } else {
             more = false;
-            if (total > 0.0) break;
+            if (total > 0.0 || total != total) break;
             w.kind = ALL;                                            // no rejection at this node, or nothing is left of its row
         }
         z = total = sum_all<C>(sh, w, lo, hi, turn);
         turn ^= 1;
         if (!more) break;
         if (w.kind == CHOSEN) {
+            if (odd_child(sh, w)) z = total = NAN;
             const int next = first_kept(sh, w, c, total);
             if (next < n) step_to(next); else more = false;
         } else more = total > 0.0;

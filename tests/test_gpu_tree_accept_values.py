@@ -1,0 +1,88 @@
+"""Acceptance on trees where p or q holds what no distribution has: a row with a NaN or +inf gives no token, however its drafts fared."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_tree_accept import Round, kb  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _rejecting(seed, V, drawn, requests):
+    """Requests whose row 0 has three children, none of which can be kept: p has nothing at their tokens."""
+    r = Round(seed, [[-1, 0, 0, 0, 1]] * requests, V, drawn)
+    for b in range(requests):
+        s = int(r.start[b])
+        r.token[s + 1:s + 4] = np.array([5, 7, 11]) % V + b % 3     # three tokens, apart from one another
+        r.p[s, r.token[s + 1:s + 4]] = 0.0
+        if drawn:
+            r.q[s, r.token[s + 1:s + 4]] = 0.1
+    return r
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("value", [np.nan, -np.nan, np.inf])
+@pytest.mark.parametrize("V", [40, 700, 33000])
+def test_one_value_of_p_that_is_not_finite(kb, drawn, value, V):  # noqa: F811
+    """At a token of the first, the second or the last child, at another one, at the ends: rejections or not, no token."""
+    at = [lambda r, s: r.token[s + 1], lambda r, s: r.token[s + 2], lambda r, s: r.token[s + 3], lambda r, s: 20, lambda r, s: 0, lambda r, s: V - 1]
+    r = _rejecting(V, V, drawn, 2 * len(at) + 1)
+    for b in range(len(at)):
+        s = int(r.start[b])
+        x = at[b](r, s)
+        r.p[s, x] = value
+        if np.isposinf(value) and b < 3 and (drawn or b == 0):       # a child whose weight is infinite is kept if it is tested before any sum is
+            r.u[s + 1:s + 4] = np.nan
+        s = int(r.start[len(at) + b])                                # no child is tested
+        r.token[s + 1:s + 4] = -1
+        r.p[s, min(x, V - 1)] = value
+    path, kept, nxt = r.run(kb)
+    assert nxt[:-1] == [-1] * (2 * len(at)) and kept[:-1] == [0] * (2 * len(at))
+    assert (path, kept, nxt) == r.want() and 0 <= nxt[-1] < V        # the last request has nothing of the kind
+
+
+@pytest.mark.parametrize("V", [40, 700, 33000])
+def test_one_nan_of_q(kb, V):  # noqa: F811
+    """It counts from the first rejection on; a row of which no draft was rejected does not look at q."""
+    r = _rejecting(V + 1, V, True, 9)
+    for b in range(4):
+        s = int(r.start[b])
+        r.q[s, (int(r.token[s + 1]), int(r.token[s + 3]), 20, V - 1)[b]] = np.nan
+        s = int(r.start[4 + b])
+        r.token[s + 1:s + 4] = -1
+        r.q[s, (0, 20, 30, V - 1)[b]] = np.nan
+    path, kept, nxt = r.run(kb)
+    assert nxt[:4] == [-1] * 4 and all(0 <= t < V for t in nxt[4:]) and kept == [0] * 9
+    assert (path, kept, nxt) == r.want()
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_a_row_that_is_left_by_its_first_draft_is_not_looked_at(kb, drawn):  # noqa: F811
+    r = Round(5, [[-1, 0, 0, 1, 1]] * 3, 900, drawn)
+    for b in range(3):
+        s = int(r.start[b])
+        r.u[s:s + 5] = 0.0
+        r.token[s + 1:s + 5] = [3, 4, 5, 6]
+        r.p[s, 3], r.p[s + 1, 5:7] = 0.5, 0.0                        # row 1 is kept, rows 3 and 4 are not
+        r.p[s, 800] = np.nan
+        if drawn:
+            r.q[s, 3], r.q[s, 900 - 1] = 0.5, np.nan
+    r.p[int(r.start[1]) + 1, 17] = np.nan                            # the row that the token comes from
+    if drawn:
+        r.q[int(r.start[2]) + 1, 17] = np.nan
+    path, kept, nxt = r.run(kb)
+    assert kept == [1, 1, 1] and nxt[1] == -1 and 0 <= nxt[0] < 900 and (nxt[2] == -1) == drawn
+    assert (path, kept, nxt) == r.want()
+
+
+def test_no_draft_is_kept_behind_a_sum_that_is_nan(kb):  # noqa: F811
+    """Chosen drafts: the NaN at the second child's token is no part of the sum that the third one would be held against."""
+    r = Round(6, [[-1, 0, 0, 0]] * 2, 300, False)
+    for b in range(2):
+        s = int(r.start[b])
+        r.token[s + 1:s + 4] = [3, 4, 5]
+        r.p[s, 3:6] = [0.0, np.nan if b == 0 else 0.0, 0.5]
+        r.u[s:s + 4] = 0.1
+    path, kept, nxt = r.run(kb)
+    assert kept == [0, 1] and nxt[0] == -1 and path[4:6] == [0, 3]
+    assert (path, kept, nxt) == r.want()
