@@ -50,6 +50,7 @@ template <int C> struct AcceptShared {
     double part[ACC_NW];
     float p_of[ACC_ROWS], q_of[ACC_ROWS], u[ACC_ROWS];               // of each row: its parent's p and q at its token, its uniform
     int parent[ACC_ROWS], token[ACC_ROWS];                           // parent -1: not to be tested
+    double sums[ACC_ROWS];                                           // of the rejections so far: the sum that the draft was held against; FAR: the one before over it
 };
 
 __device__ __forceinline__ double warp_sum64(double v) {
@@ -76,13 +77,30 @@ __device__ __forceinline__ int next_child(const int *parent, int n, int node, in
     return n;
 }
 
-// What a row's weights are: its values; what rejections of drafts drawn from q have left, which is max(0, a p - b q) whatever their number (max(0, y) / Z - q and
-// y / Z - q have the same positive part); its values without those of the children of `node`.
-enum { ALL = 0, DRAWN = 1, CHOSEN = 2 };
-struct Weights { const float *p, *q; int kind, node, n; double a, b; };
-__device__ __forceinline__ double left_of(double a, double b, float p, float q) {
-    const double x = fma(a, (double)p, -b * (double)q);
-    return x < 0.0 ? 0.0 : x;                                        // NaN stays
+// What a row's weights are: its values; what rejections of drafts drawn from q have left; its values without those of the children of `node`.
+// Drafts drawn.  DRAWN: W = max(0, p - r q), r the sum of the sums S that the rejected drafts were held against (S = 1 at first): with W = S' w, S' the sum before, a draft is kept
+// iff u S q < W, and W / S - q is positive where p - (r + S) q is.  One pass whatever came before, but each rejection makes S smaller by its Z, and the digits of p - r q that are
+// left are those of r: it is held in two doubles.  While S >= SMALL they hold it exactly: an S ends at 2^-93, r is below 2^11.  FAR: below that (two dozen children that
+// were rejected with a Z of a third, which drawn drafts are with a probability of SMALL) the recursion itself, w <- max(0, w / Z - q), `times` steps a value.
+enum { ALL = 0, DRAWN = 1, CHOSEN = 2, FAR = 3 };
+constexpr double SMALL = 0x1p-40;
+struct Weights { const float *p, *q; int kind, node, n; double r, r_low; int times; double *sums; };
+__device__ __forceinline__ double positive(double x) { return x < 0.0 ? 0.0 : x; }           // NaN stays
+__device__ __forceinline__ double left_of(double r, double r_low, float p, float q) { return positive(fma(-r_low, (double)q, fma(-r, (double)q, (double)p))); }
+__device__ __forceinline__ double far_left_of(const double *over_z, int times, float p, float q) {
+    double x = p;
+#pragma unroll 1
+    for (int k = 0; k < times; ++k) x = positive(fma(x, over_z[k], -(double)q));
+    return x;
+}
+__device__ __forceinline__ double drawn_left_of(const Weights &w, float p, float q) {
+    return w.kind == FAR ? far_left_of(w.sums, w.times, p, q) : left_of(w.r, w.r_low, p, q);
+}
+// r + s, to the last bit of its second double.
+__device__ __forceinline__ void add_to(double &r, double &r_low, double s) {
+    const double sum = r + s, of_s = sum - r, low = (r - (sum - of_s)) + (s - of_s) + r_low;
+    r = sum + low;
+    r_low = low - (r - sum);
 }
 template <int C> __device__ __forceinline__ int child_token(const AcceptShared<C> &sh, const Weights &w, int i) { return i < w.n && sh.parent[i] == w.node ? sh.token[i] : -1; }
 
@@ -136,7 +154,7 @@ static __device__ __noinline__ double sum_values(const float *p, int i0, int i1,
         for (int j = i; j < min(i + 4, i1); ++j) t += j == out0 || j == out1 || j == out2 || j == out3 ? 0.0 : (double)p[j];
     return t;
 }
-static __device__ __noinline__ double sum_left(const float *p, const float *q, double a, double b, int i0, int i1) {
+static __device__ __noinline__ double sum_left(const float *p, const float *q, double r, double r_low, int i0, int i1) {
     constexpr int N = 2;
     double s[2] = {0.0, 0.0};
     unsigned top = 0;
@@ -154,16 +172,22 @@ static __device__ __noinline__ double sum_left(const float *p, const float *q, d
         for (int e = 0; e < N; ++e)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const double x = fma(a, scaled(v[e][j]), -b * scaled(u[e][j]));
+                const double y = scaled(u[e][j]), x = fma(-r_low, y, fma(-r, y, scaled(v[e][j])));
                 s[j & 1] += __double2hiint(x) < 0 ? 0.0 : x;
                 top = max(top, u[e][j]);
             }
     }
-    if (top < 0x7f800000u && s[0] + s[1] < a * TOO_LARGE) return (s[0] + s[1]) * SCALED_BACK;
+    if (top < 0x7f800000u && s[0] + s[1] < TOO_LARGE) return (s[0] + s[1]) * SCALED_BACK;
     double t = 0.0;
 #pragma unroll 1
     for (int i = first; i < i1; i += 128)
-        for (int j = i; j < min(i + 4, i1); ++j) t += left_of(a, b, p[j], q[j]);
+        for (int j = i; j < min(i + 4, i1); ++j) t += left_of(r, r_low, p[j], q[j]);
+    return t;
+}
+static __device__ __noinline__ double sum_far(const float *p, const float *q, const double *over_z, int times, int i0, int i1) {
+    double t = 0.0;
+#pragma unroll 1
+    for (int i = i0 + (threadIdx.x & 31); i < i1; i += 32) t += far_left_of(over_z, times, p[i], q[i]);
     return t;
 }
 // Whether an id is the token of a child, for the 32 ids from `base` on.
@@ -186,9 +210,9 @@ template <int C> __device__ __forceinline__ int next_token(const AcceptShared<C>
 }
 // The sum of the weights of ids [i0, i1), by a warp.
 template <int C> __device__ __forceinline__ double sum_of(const AcceptShared<C> &sh, const Weights &w, int i0, int i1) {
-    const int lane = threadIdx.x & 31;
     double s = 0.0;
-    if (w.kind == DRAWN) s = sum_left(w.p, w.q, w.a, w.b, i0, i1);
+    if (w.kind == DRAWN) s = sum_left(w.p, w.q, w.r, w.r_low, i0, i1);
+    else if (w.kind == FAR) s = sum_far(w.p, w.q, w.sums, w.times, i0, i1);
     else {
         for (int from = i0, to; from < i1; from = to) {              // runs of ids with OUTS of the children's tokens among them, or all
             int out[OUTS];
@@ -275,7 +299,7 @@ template <int C> __device__ __forceinline__ int find_id(AcceptShared<C> &sh, con
     }
     const int base = lo + 32 * warp, id = base + lane;               // an id a thread
     double x = 0.0;
-    if (id < hi) x = w.kind == DRAWN ? left_of(w.a, w.b, w.p[id], w.q[id]) : (double)w.p[id];
+    if (id < hi) x = w.kind == DRAWN || w.kind == FAR ? drawn_left_of(w, w.p[id], w.q[id]) : (double)w.p[id];
     if (w.kind == CHOSEN && childs_id(sh, w, base)) x = 0.0;
     const double upto = warp_upto64(x);
     __syncthreads();
@@ -336,7 +360,7 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
     const int S = ((V + C - 1) / C + 31) & ~31;                      // ids of a block
     auto first_id = [&](int r) { return (int)min((long long)V, (long long)r * S); };
     const int lo = first_id(rank), hi = first_id(rank + 1);
-    Weights w{a.p + (size_t)row0 * V, a.q ? a.q + (size_t)row0 * V : nullptr, ALL, 0, n, 1.0, 0.0};
+    Weights w{a.p + (size_t)row0 * V, a.q ? a.q + (size_t)row0 * V : nullptr, ALL, 0, n, 0.0, 0.0, 0, sh.sums};
     const float u_final = a.u_final[b];
     for (int i = tid; i < n; i += ACC_NT) {
         const int up = a.parent[row0 + i], x = a.token[row0 + i];
@@ -370,22 +394,30 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
         w.q = a.q ? a.q + row : nullptr;
         w.kind = ALL;
         w.node = last = c;
-        w.a = z = 1.0;
-        w.b = 0.0;
+        w.r = w.r_low = 0.0;
+        w.sums += w.times;                                           // no place of them is written twice: some warp may still be at the test before
+        w.times = 0;
+        z = 1.0;
         total = -1.0;
     };
     for (bool more = true; n > 0;) {                                 // more: there may be children that can be kept
         const int c = more ? next_child(sh.parent, n, w.node, last) : n;
         if (c < n) {
             last = c;
-            const double mine = w.kind == DRAWN ? left_of(w.a, w.b, sh.p_of[c], sh.q_of[c]) : (double)sh.p_of[c];
+            const double mine = w.kind == DRAWN || w.kind == FAR ? drawn_left_of(w, sh.p_of[c], sh.q_of[c]) : (double)sh.p_of[c];
             if ((double)sh.u[c] * z * (double)sh.q_of[c] < mine) {
                 step_to(c);
                 continue;
             }
-            w.kind = a.q ? DRAWN : CHOSEN;
-            w.a /= z;
-            w.b = w.b / z + 1.0;
+            if (a.q) {
+                if (tid == 0) w.sums[w.times] = w.kind == FAR ? 1.0 / z : z;
+                ++w.times;
+                if (w.kind == FAR) __syncthreads();
+                else {
+                    w.kind = DRAWN;
+                    add_to(w.r, w.r_low, z);
+                }
+            } else w.kind = CHOSEN;
         } else {
             more = false;
             if (total > 0.0 || total != total) break;
@@ -398,6 +430,23 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
             if (odd_child(sh, w)) z = total = NAN;
             const int next = first_kept(sh, w, c, total);
             if (next < n) step_to(next); else more = false;
+        } else if (w.kind == DRAWN && total < SMALL) {               // once more, by the recursion
+            __syncthreads();
+            double over_z[ACC_ROWS / ACC_NT];
+#pragma unroll
+            for (int i = 0; i < ACC_ROWS / ACC_NT; ++i) {
+                const int k = i * ACC_NT + tid;
+                over_z[i] = k < w.times ? (k > 0 ? w.sums[k - 1] : 1.0) / w.sums[k] : 0.0;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < ACC_ROWS / ACC_NT; ++i)
+                if (i * ACC_NT + tid < w.times) w.sums[i * ACC_NT + tid] = over_z[i];
+            __syncthreads();
+            w.kind = FAR;
+            z = total = sum_all<C>(sh, w, lo, hi, turn);
+            turn ^= 1;
+            more = total > 0.0;
         } else more = total > 0.0;
     }
     if (n > 0) {

@@ -86,3 +86,37 @@ def test_no_draft_is_kept_behind_a_sum_that_is_nan(kb):  # noqa: F811
     path, kept, nxt = r.run(kb)
     assert kept == [0, 1] and nxt[0] == -1 and path[4:6] == [0, 3]
     assert (path, kept, nxt) == r.want()
+
+
+@pytest.mark.parametrize("V", [2, 33, 5000])
+@pytest.mark.parametrize("children", [12, 40, 400, 1000])
+def test_many_rejections_at_one_row(kb, V, children):  # noqa: F811
+    """All children are the token of which p has less than q.  After the first rejection only ids behind it have weight, in shares that every further one leaves as they are
+    up to q: Z is small each time, and what is left of a row stays exact to some 2^-50 however often."""
+    r = Round(8, [[-1] + [0] * children] * 4, V, True)
+    for b, (top, more) in enumerate([(0.9, 0.05), (0.99, 0.005), (0.5, 0.25), (0.999, 1e-6)]):
+        s = int(r.start[b])
+        r.q[s], r.p[s] = 0.0, 0.0
+        r.q[s, 0], r.q[s, 1] = top, 1 - top
+        r.p[s, 0], r.p[s, 1] = top + more, 1 - top - more
+        if V > 2:
+            r.q[s, 0], r.q[s, 20] = top / 2, top / 2
+            r.p[s, 0], r.p[s, 20] = top / 2 + more, top / 2
+        r.token[s + 1:s + 1 + children], r.u[s:s + 1 + children] = 1, np.float32(1 - 2 ** -24)
+        r.last[b] = np.float32(1 - 2 ** -24)
+    path, kept, nxt = r.run(kb)
+    assert kept == [0] * 4 and nxt == [0] * 4                        # token 0 is all that is ever left
+    assert (path, kept, nxt) == r.want()
+
+
+def test_siblings_of_drafts_that_are_next_to_p(kb):  # noqa: F811
+    """q so near p that the first rejections leave next to nothing; many drafts, not only drawn ones.  The oracle's decisions throughout."""
+    rng = np.random.default_rng(3)
+    for seed in range(12):
+        V = int(rng.choice([3, 8, 60, 1000]))
+        r = Round(40 + seed, [[-1] + [0] * 30 + [5] * 10] * 20, V, True, sharp=2, zeros=0.1, mix=1.0)
+        r.p = (r.q * (1 + 10.0 ** -rng.integers(1, 6) * rng.standard_normal(r.q.shape))).astype(np.float32)
+        r.p /= r.p.sum(1, keepdims=True)
+        r.token = np.where(rng.random(len(r.token)) < 0.7, rng.integers(0, V, len(r.token)), r.token)
+        r.u = np.where(rng.random(len(r.u)) < 0.8, np.float32(1 - 2 ** -20), r.u).astype(np.float32)
+        assert r.run(kb) == r.want()
