@@ -49,7 +49,7 @@ template <int C> struct AcceptShared {
     double slot[2][C * ACC_NW];                                      // the sums of all blocks' warps; the next pass's may come while these are read
     double part[ACC_NW];
     float p_of[ACC_ROWS], q_of[ACC_ROWS], u[ACC_ROWS];               // of each row: its parent's p and q at its token, its uniform
-    int parent[ACC_ROWS], token[ACC_ROWS];                           // parent -1: not to be tested
+    alignas(16) int parent[ACC_ROWS], token[ACC_ROWS];                           // parent -1: not to be tested
     double sums[ACC_ROWS];                                           // of the rejections so far: the sum that the draft was held against; FAR: the one before over it
 };
 
@@ -310,15 +310,39 @@ template <int C> __device__ __forceinline__ int find_id(AcceptShared<C> &sh, con
     return past ? base + __ffs(past) - 1 : some ? base + 31 - __clz(some) : base;
 }
 
-// Whether p at the token of one of the node's children is not finite: the sum without the children does not show it.  The same in every warp.
-template <int C> __device__ __forceinline__ bool odd_child(const AcceptShared<C> &sh, const Weights &w) {
-    bool odd = false;
-    for (int i = threadIdx.x & 31; i < w.n; i += 32) odd |= sh.parent[i] == w.node && !isfinite(sh.p_of[i]);
-    return __any_sync(0xffffffffu, odd);
+// FAR's factors from the sums of a node's rejections, by a block.
+static __device__ __noinline__ void recur(double *sums, int times) {
+    static_assert(ACC_ROWS == 4 * ACC_NT, "four a thread");
+    double f[4];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = i * ACC_NT + threadIdx.x;
+        f[i] = k < times ? (k > 0 ? sums[k - 1] : 1.0) / sums[k] : 0.0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i * ACC_NT + threadIdx.x < times) sums[i * ACC_NT + threadIdx.x] = f[i];
+    __syncthreads();
+}
+// Whether a sibling before row i has its token.  Siblings lie behind their parent: a chain has none to look at.  A piece of code of its own, for the registers of the rest.  A call
+// with 1024 rows of 32000 ids as a chain / all children of one 23 / 85 us (every pair of rows, a division each: 432 / 500).
+static __device__ __noinline__ bool came_before(const int *parent, const int *token, int i) {
+    const int up = parent[i], x = token[i];
+    bool found = false;
+#pragma unroll 2
+    for (int j = (up + 1) & ~3; j < i; j += 4) {
+        const int4 p = *reinterpret_cast<const int4 *>(parent + j), t = *reinterpret_cast<const int4 *>(token + j);
+        found |= (p.x == up && t.x == x) || (j + 1 < i && p.y == up && t.y == x) || (j + 2 < i && p.z == up && t.z == x) || (j + 3 < i && p.w == up && t.w == x);
+    }
+    return found;
 }
 // Drafts chosen: of the children of w.node behind row c, which was rejected, the first that is kept; `rest`: the sum without all of the node's children.  n: none is.
-// The sum that a child is held against is the rest and the children from it on: all are tested at once.  The same in every warp.
-template <int C> __device__ __forceinline__ int first_kept(const AcceptShared<C> &sh, const Weights &w, int c, double rest) {
+// The sum that a child is held against is the rest and the children from it on: all are tested at once.  The same in every warp.  Where p at a child's token is not finite
+// the rest becomes NaN: the children before that one are held against such a sum, those behind it would not be.
+template <int C> __device__ __forceinline__ int first_kept(const AcceptShared<C> &sh, const Weights &w, int c, double &rest) {
+    if (!isfinite(sh.p_of[c])) rest = NAN;
     const int lane = threadIdx.x & 31;
     auto p_of = [&](int i) { return i > c && i < w.n && sh.parent[i] == w.node ? (double)sh.p_of[i] : 0.0; };
     auto from_here_on = [&](double v) {                              // the sum over this lane and those behind it
@@ -342,6 +366,10 @@ template <int C> __device__ __forceinline__ int first_kept(const AcceptShared<C>
         const int i = 32 * k + lane;
         const double mine = p_of(i), sum = rest + __shfl_sync(0xffffffffu, later, k) + from_here_on(mine);
         const unsigned found = __ballot_sync(0xffffffffu, i > c && i < w.n && sh.parent[i] == w.node && (double)sh.u[i] * sum < mine);
+        if (__any_sync(0xffffffffu, !isfinite(mine))) {
+            rest = NAN;
+            break;
+        }
         if (found) return 32 * k + __ffs(found) - 1;
     }
     return w.n;
@@ -376,10 +404,8 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
         for (int i = tid; i < n_all; i += ACC_NT) a.path[row0 + i] = i == 0 ? 0 : -1;
     __syncthreads();
     if (!a.q) {                                                      // a token that a sibling before it has: nothing is left of it when it is tested
-        for (int t = tid; t < n * n; t += ACC_NT) {
-            const int i = t / n, j = t % n;
-            if (j < i && sh.parent[i] >= 0 && sh.parent[j] == sh.parent[i] && sh.token[j] == sh.token[i]) sh.p_of[i] = 0.f;
-        }
+        for (int i = tid; i < n; i += ACC_NT)
+            if (sh.parent[i] >= 0 && came_before(sh.parent, sh.token, i)) sh.p_of[i] = 0.f;
         __syncthreads();
     }
     if (C > 1) cluster.barrier_wait();
@@ -423,30 +449,17 @@ template <int C> __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(ACC
             if (total > 0.0 || total != total) break;
             w.kind = ALL;                                            // no rejection at this node, or nothing is left of its row
         }
-        z = total = sum_all<C>(sh, w, lo, hi, turn);
-        turn ^= 1;
-        if (!more) break;
-        if (w.kind == CHOSEN) {
-            if (odd_child(sh, w)) z = total = NAN;
-            const int next = first_kept(sh, w, c, total);
-            if (next < n) step_to(next); else more = false;
-        } else if (w.kind == DRAWN && total < SMALL) {               // once more, by the recursion
-            __syncthreads();
-            double over_z[ACC_ROWS / ACC_NT];
-#pragma unroll
-            for (int i = 0; i < ACC_ROWS / ACC_NT; ++i) {
-                const int k = i * ACC_NT + tid;
-                over_z[i] = k < w.times ? (k > 0 ? w.sums[k - 1] : 1.0) / w.sums[k] : 0.0;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < ACC_ROWS / ACC_NT; ++i)
-                if (i * ACC_NT + tid < w.times) w.sums[i * ACC_NT + tid] = over_z[i];
-            __syncthreads();
-            w.kind = FAR;
+        for (;;) {
             z = total = sum_all<C>(sh, w, lo, hi, turn);
             turn ^= 1;
-            more = total > 0.0;
+            if (w.kind != DRAWN || !(total < SMALL)) break;
+            recur(w.sums, w.times);                                  // once more, by the recursion
+            w.kind = FAR;
+        }
+        if (!more) break;
+        if (w.kind == CHOSEN) {
+            const int next = first_kept(sh, w, c, total);
+            if (next < n) step_to(next); else more = false;
         } else more = total > 0.0;
     }
     if (n > 0) {

@@ -120,3 +120,61 @@ def test_siblings_of_drafts_that_are_next_to_p(kb):  # noqa: F811
         r.token = np.where(rng.random(len(r.token)) < 0.7, rng.integers(0, V, len(r.token)), r.token)
         r.u = np.where(rng.random(len(r.u)) < 0.8, np.float32(1 - 2 ** -20), r.u).astype(np.float32)
         assert r.run(kb) == r.want()
+
+
+@pytest.mark.parametrize("at", [1, 20, 31, 32, 40, 70])
+def test_a_nan_among_many_chosen_drafts(kb, at):  # noqa: F811
+    """Children in several groups of 32 rows; the one at `at` has the NaN, the last one all the weight there is."""
+    n = 72
+    r = Round(9, [[-1] + [0] * (n - 1)] * 2, 500, False)
+    for b in range(2):
+        s = int(r.start[b])
+        r.token[s + 1:s + n] = np.arange(1, n)
+        r.p[s, 1:n - 1], r.p[s, n - 1] = 0.0, 0.5
+        r.u[s:s + n] = 0.9
+        r.u[s + n - 1] = 0.25
+    r.p[int(r.start[0]), at] = np.nan
+    path, kept, nxt = r.run(kb)
+    assert kept == [0, 1] and nxt[0] == -1 and path[n + 1] == n - 1
+    assert (path, kept, nxt) == r.want()
+
+
+@pytest.mark.parametrize("at", [[2, 3], [4, 37], [33, 1000], [1, 2, 3, 4, 1023]])
+def test_tokens_that_come_again_among_many_rows(kb, at):  # noqa: F811
+    """Chosen drafts: of siblings with one token the first one counts, the others have nothing left.  All rows are row 0's children, or of two parents in turn."""
+    n = 1024
+    for parents in ([-1] + [0] * (n - 1), [-1, 0] + [i % 2 for i in range(n - 2)]):
+        r = Round(10, [parents], 3000, False)
+        r.token[1:] = np.arange(1, n)
+        r.token[at] = 2000
+        r.p[:] = 1.0 / 3000
+        r.u[:] = np.float32(1 - 2 ** -24)
+        r.u[at[1:]] = 0.0                                            # kept whatever is left
+        got = r.run(kb)
+        assert got == r.want()
+
+
+def test_rows_without_siblings_cost_little(kb):  # noqa: F811
+    """Chosen drafts: a chain of 1024 rows has no siblings to compare, 16 times as many rows as one of 64 must not take 256 times as long."""
+    took = []
+    for n in (64, 1024):
+        r = Round(12, [list(range(-1, n - 1))], 1000, False, mix=0.0)
+        args, out = r.on_device(), [torch.zeros(k, dtype=torch.int32, device="cuda") for k in (n, 1, 1)]
+        args[5].fill_(1.0)                                           # nothing is kept: what the rows cost, not the path
+        kb.knnssd_tree_accept(*args, *out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(20):
+                kb.knnssd_tree_accept(*args, *out)
+        e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        times = []
+        for _ in range(7):
+            e[0].record()
+            graph.replay()
+            e[1].record()
+            torch.cuda.synchronize()
+            times.append(e[0].elapsed_time(e[1]))
+        took.append(np.median(times))
+        assert out[1].tolist() == [0]
+    assert took[1] < 12 * took[0]
