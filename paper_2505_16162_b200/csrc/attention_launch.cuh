@@ -122,20 +122,28 @@ template <int HD, bool PAGED, bool TREE = false> knnssd_status launch_tensor(att
 }
 
 // Trees over short contexts: whether a block for 16 rows and all positions that the table has room for is the sooner way, and with how many warps (0: it is not), by microseconds that were
-// measured.  A block of eight warps, one a processor at a time, takes 3 and, for 128 positions of 128 dimensions, 0.8 (bf16), 1.45 (fp32 rows, bf16 pages) or 2.4 (fp32; contexts that
-// fill two thirds of their tables); of four warps, two a processor, 3.5 and 2.2 times that.  The ways that share positions out take 16 to 25 whatever the sizes and then some 7 GB of
-// bf16 pages a millisecond, half of that of fp32 ones.  8 / 4 warps / shared out: one request of 48 rows, 32 bf16 heads and 300 positions 10 / 14 / 24 us, 8 requests of 12 rows 18 / 14 / 34;
-// 32 requests of 60 positions 36 / - / 30.
+// measured.
+// bf16 pages: a block of eight warps, one a processor at a time, takes 3 and, for 128 positions of 128 dimensions, 0.8 (bf16 rows) or 1.45 (fp32); of four warps, two a processor, 3.5 and
+// 2.2 times that.  The ways that share positions out take 16 to 20 whatever the sizes and then some 7 GB of pages a millisecond.  8 / 4 warps / shared out: one request of 48
+// rows, 32 bf16 heads and 300 positions 10 / 14 / 24 us, 8 requests of 12 rows 18 / 14 / 34; 32 requests of 60 positions 36 / - / 30.
+// fp32 pages: always eight warps; 1 and, for each round of blocks (between their number a processor and that rounded up, as processors end apart), 2 and 2.4 for 128 positions of
+// 128 dimensions, 0.7 of that for 64.  Shared out 23 (64 dimensions: 16) and 1.5 a block of a processor for the same.  Over 570 calls of 1 to 90 requests, tables of 32 to 2048 positions, full
+// or not, the way taken is 1.5 % longer than the sooner one, at most 1.5 times as long.  Whole / shared out: 22 requests of 64 rows, 8 heads on 2 of 64 dimensions, 80 positions 22 / 24 us; 3 of 48,
+// 32 heads on 4, 480 positions 35 / 44; 1 of 8, 40 heads, 1472 positions 42 / 27; 5 of 2, 32 heads, 1424 positions 88 / 68.
 inline int short_warps(attn::Args a, int dtype, int cache_dtype, int hd) {
     share_heads(a, treerows::ROWS);
     const long long positions = (long long)a.max_pages << a.page_shift, tiles = (long long)a.R / a.tb + a.B;
     const double blocks = (double)tiles * a.nvh / sm_count();
     if (blocks > 8.0 || positions > 2048) return 0;                  // beyond what the figures are of
-    const double step = hd / 128.0 * (cache_dtype == 0 ? 2.4 : dtype == 0 ? 1.45 : 0.8) * positions / 128.0;
+    if (cache_dtype == 0) {
+        const double part = (hd == 64 ? 0.7 : 1.0) * positions / 128.0, rounds = (std::ceil(blocks) + std::max(1.0, blocks)) / 2;
+        return 1.0 + rounds * (2.0 + 2.4 * part) < (hd == 64 ? 16.0 : 23.0) + 1.5 * blocks * part ? 8 : 0;
+    }
+    const double step = hd / 128.0 * (dtype == 0 ? 1.45 : 0.8) * positions / 128.0;
     const double eight = 3.0 + std::ceil(blocks) * (3.0 + step), four = 3.0 + std::max(1.0, blocks / 2) * (3.5 + 2.2 * step);
-    const double shared = (dtype == 0 && hd == 64 ? 16.0 : cache_dtype == 0 ? 25.0 : 20.0) + (double)a.B * a.KV * positions * hd * (cache_dtype == 0 ? 16.0 : 4.0) / 7e6;
+    const double shared = (dtype == 0 && hd == 64 ? 16.0 : 20.0) + (double)a.B * a.KV * positions * hd * 4.0 / 7e6;
     if (std::min(eight, four) >= shared) return 0;
-    return eight <= four || cache_dtype == 0 ? 8 : 4;
+    return eight <= four ? 8 : 4;
 }
 template <int HD, typename QT, typename KT, int W> knnssd_status launch_short_of(attn::Args a, cudaStream_t s) {
     using L = treerows::Lay<HD, QT, KT, W>;
