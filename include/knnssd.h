@@ -489,8 +489,11 @@ knnssd_status knnssd_attention_status(void *cuda_stream);
 
 /*
  * Test hook: in attention of bf16 rows launched by this process from now on, every block's copies end after `tiles` tiles and waits give up after
- * spin_limit polls (1 .. 1000000, else KNNSSD_ERR_INVALID_ARG).  spin_limit 0: as before.  Nothing faults or hangs.
+ * spin_limit polls (1 .. 1000000, else KNNSSD_ERR_INVALID_ARG).  spin_limit 0: as before.  Nothing faults or hangs.  Over pages two warps of a block share the copies of each
+ * tile: tiles | KNNSSD_DEBUG_ONLY_FIRST, tiles | KNNSSD_DEBUG_ONLY_SECOND end only one's, the other goes on until it gives up.
  */
+#define KNNSSD_DEBUG_ONLY_FIRST (1u << 30)
+#define KNNSSD_DEBUG_ONLY_SECOND (1u << 31)
 knnssd_status knnssd_debug_attention_timeout(unsigned spin_limit, unsigned tiles);
 
 /* ---- drafts that branch ----

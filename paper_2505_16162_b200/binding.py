@@ -447,8 +447,12 @@ def knnssd_attention_status(device: Optional[int] = None) -> None:
     _call(_lib.knnssd_attention_status, "knnssd_attention_status", torch.cuda.current_device() if device is None else device)
 
 
+KNNSSD_DEBUG_ONLY_FIRST, KNNSSD_DEBUG_ONLY_SECOND = 1 << 30, 1 << 31
+
+
 def knnssd_debug_attention_timeout(spin_limit: int, tiles: int = 0) -> None:
-    """Test hook: attention of bf16 rows loses its copies after `tiles` tiles and gives up after spin_limit polls; 0: as before."""
+    """Test hook: attention of bf16 rows loses its copies after `tiles` tiles and gives up after spin_limit polls; 0: as before.  tiles | KNNSSD_DEBUG_ONLY_FIRST (_SECOND): over
+    pages, the copies of one of the two warps that share them."""
     rc = _lib.knnssd_debug_attention_timeout(spin_limit, tiles)
     if rc:
         raise KnnssdError(rc, "knnssd_debug_attention_timeout")

@@ -34,9 +34,9 @@ struct Args {
     struct Part *parts;
     float2 *ml;
     float *o;
-    // bounded waits (tensor kernel): where one that gives up leaves its code, after how many polls; tiles that a block's copies end after
+    // bounded waits (tensor kernel): where one that gives up leaves its code, after how many polls; tiles that a block's copies end after, those of each of the copying warps
     int *err;
-    unsigned wait_limit, stop_after;
+    unsigned wait_limit, stop_after[2];
     const unsigned long long *seen;       // trees: [R], which of the 64 positions up to a row's own it sees
 };
 

@@ -18,8 +18,8 @@ namespace knnssd {
 
 // The word of the current device that the bounded waits of the tensor-core attention report to, until knnssd_attention_status takes it.
 int *attention_err_ptr();
-// What knnssd_debug_attention_timeout sets: polls of a wait, tiles that a block's copies end after.
-extern std::atomic<unsigned> g_wait_limit, g_stop_after;
+// What knnssd_debug_attention_timeout sets: polls of a wait, tiles that the copies of a block's first and second copying warp end after.
+extern std::atomic<unsigned> g_wait_limit, g_stop_after[2];
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool power_of_two(int v) { return v > 0 && (v & (v - 1)) == 0; }
@@ -85,7 +85,7 @@ template <int HD, bool PAGED, bool TREE = false> knnssd_status launch_tensor(att
     static bool configured[kMaxDevices] = {};
     const auto kernel = tcattn::tensor_kernel<HD, PAGED, TREE>;
     a.err = attention_err_ptr();
-    a.wait_limit = g_wait_limit; a.stop_after = g_stop_after;
+    a.wait_limit = g_wait_limit; a.stop_after[0] = g_stop_after[0]; a.stop_after[1] = g_stop_after[1];
     if (!a.err || !allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
     share_heads(a, tcattn::HALF_ROWS);
     const int ctas = sm_count();

@@ -12,7 +12,7 @@
 
 using namespace knnssd;
 
-std::atomic<unsigned> knnssd::g_wait_limit{tcattn::WAIT_LIMIT}, knnssd::g_stop_after{~0u};
+std::atomic<unsigned> knnssd::g_wait_limit{tcattn::WAIT_LIMIT}, knnssd::g_stop_after[2]{~0u, ~0u};
 
 namespace {
 
@@ -137,7 +137,9 @@ knnssd_status knnssd_attention_status(void *cuda_stream) {
 knnssd_status knnssd_debug_attention_timeout(unsigned spin_limit, unsigned tiles) {
     if (spin_limit > tcattn::WAIT_LIMIT) return KNNSSD_ERR_INVALID_ARG;
     g_wait_limit = spin_limit ? spin_limit : tcattn::WAIT_LIMIT;
-    g_stop_after = spin_limit ? tiles : ~0u;
+    const unsigned only = tiles & (KNNSSD_DEBUG_ONLY_FIRST | KNNSSD_DEBUG_ONLY_SECOND), after = tiles & ~only;
+    g_stop_after[0] = spin_limit && only != KNNSSD_DEBUG_ONLY_SECOND ? after : ~0u;
+    g_stop_after[1] = spin_limit && only != KNNSSD_DEBUG_ONLY_FIRST ? after : ~0u;
     return KNNSSD_OK;
 }
 

@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(threads_of(PAGED), 1) tensor_kernel(const __gr
                 const bool own = job.paired && job.n[0] > 0 && job.n[1] > 0;
                 const int T = job.tiles, total_tiles = (own ? 4 : 2) * T;
                 if (PAGED && T) { id = page_of(job.j0); next_id = page_of(job.j0 + 1); }
-                const int until = (int)min((unsigned)total_tiles, a.stop_after - fills);      // fewer in a test of the waits alone
+                const int until = (int)min((unsigned)total_tiles, a.stop_after[loader] - fills);      // fewer in a test of the waits alone
 #pragma unroll 1
                 for (int i = 0; i < until && ok; ++i) {
                     // half i's q before tile i: the first K is on its way while q waits for the products of the item before
@@ -484,9 +484,15 @@ __global__ void __launch_bounds__(threads_of(PAGED), 1) tensor_kernel(const __gr
                 more = it.next(a) && it.start < x1;
             }
             if (PAGED) {                                             // where one loader gave up the other's tiles still have to be full: it arrives for those that it left out
+                // (at most a turn of the ring: for a tile in a place for the second time the other has waited for its products, and they for both).  Their rows are lost.
                 if (lane == 0) filled[loader] = fills;
+                __syncwarp();
                 asm volatile("bar.sync 1, 64;" ::: "memory");
                 const unsigned all = max(filled[0], filled[1]);
+                if (fills < all && lane == 0 && !quit) {
+                    quit = 1;
+                    atomicExch(a.err, 211);
+                }
                 for (; fills < all; ++fills)
                     if (lane == 0) bar_arrive(kv_full + 8 * (fills % L::TILES));
             }
