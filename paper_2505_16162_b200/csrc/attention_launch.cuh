@@ -127,8 +127,9 @@ template <int HD, bool PAGED, bool TREE = false> knnssd_status launch_tensor(att
 // 2.2 times that.  The ways that share positions out take 16 to 20 whatever the sizes and then some 7 GB of pages a millisecond.  8 / 4 warps / shared out: one request of 48
 // rows, 32 bf16 heads and 300 positions 10 / 14 / 24 us, 8 requests of 12 rows 18 / 14 / 34; 32 requests of 60 positions 36 / - / 30.
 // fp32 pages: always eight warps; 1 and, for each round of blocks (between their number a processor and that rounded up, as processors end apart), 2 and 2.4 for 128 positions of
-// 128 dimensions, 0.7 of that for 64.  Shared out 23 (64 dimensions: 16) and 1.5 a block of a processor for the same.  Over 570 calls of 1 to 90 requests, tables of 32 to 2048 positions, full
-// or not, the way taken is 1.5 % longer than the sooner one, at most 1.5 times as long.  Whole / shared out: 22 requests of 64 rows, 8 heads on 2 of 64 dimensions, 80 positions 22 / 24 us; 3 of 48,
+// 128 dimensions, 0.7 of that for 64.  Shared out 23 (64 dimensions: 16) and 1.5 a block of a processor for the same.  Over 1500 calls of 1 to 90 requests, tables of 32 to 2048 positions, full
+// or not, the way taken is 1.3 to 2 % longer than the sooner one, where it is short and not at most 1.4 times, where it is shared out and hardly filled 1.7 times as long.  From two blocks a
+// processor on the two are within 5 % of one another on average (8 requests of 25 rows, 40 heads, 1280 positions 174 / 191: shared out).  Whole / shared out: 22 requests of 64 rows, 8 heads on 2 of 64 dimensions, 80 positions 22 / 24 us; 3 of 48,
 // 32 heads on 4, 480 positions 35 / 44; 1 of 8, 40 heads, 1472 positions 42 / 27; 5 of 2, 32 heads, 1424 positions 88 / 68.
 inline int short_warps(attn::Args a, int dtype, int cache_dtype, int hd) {
     share_heads(a, treerows::ROWS);
@@ -165,6 +166,9 @@ template <int HD> knnssd_status launch_tree_rows(attn::Args a, cudaStream_t s) {
     const auto kernel = treerows::tree_rows_kernel<HD, float, float, 0>;
     if (!allow_smem(kernel, L::SMEM, configured)) return KNNSSD_ERR_CUDA;
     share_heads(a, treerows::ROWS);
+    // As above.  extra 0 / 64 / 128 / 256 / 512: 24 requests of 13 rows and 300 to 1700 positions 202 / 193 / 186 / 189 / 204 us, 32 of 6 and 100 to 700 161 / 131 / 124 / 132 / 142, one of 25
+    // and 8000 126 / 122 / 122 / 122 / 127; least_run 64 / 128 / 256 / 512: one of 1 row and 3000 36 / 36 / 36 / 46, 3 of 48 and 900 38 / 38 / 38 / 42, two of 13 and 200 and 90 in a wide table
+    // 13 / 15 / 18 / 24 (short_warps' figures of the shared-out way are of 256), the others the same.
     a.extra = 128;
     a.least_run = 256;
     a.most = (int)std::min((long long)L::BLOCKS * sm_count(), 128ll * a.nvh * std::max(a.B, a.R / a.tb));

@@ -3,13 +3,14 @@
 // The mathematics is the rows kernel's (row_attention.cuh): up to 16 rows of a request that share a K/V head are an operand of m16n8k16 products, fp32 values are multiplied as three bf16 terms
 // each, a row sees what its word says.  Here a block has the rows: they lie in shared memory as the products take them, its warps take 16 positions each in turn, K and V straight from the pages into
 // the products' operands (any order of a head's dimensions serves a sum over them, and each is stored where it belongs), and put their parts together in shared memory.
+// Fewer bits: the weights of bf16 rows are rounded to bf16 for the product with V (2^-8 relative at most), as the tensor kernel has them; sums are fp32.
 //
 // Short contexts: a block has an item whole, one launch does it all, without scratch.  Which it has follows from row_start alone: request b's blocks are those from row_start[b] / tb + b on, as many
 // as row_start[b + 1] / tb - row_start[b] / tb + 1, which are enough for its rows whatever the requests before it have.  Bound by latency: rows, page, K and V, products, the parts.  Two requests of
 // 13 rows, 4 fp32 heads of 64 over 96 positions 5.7 us, where the ways for long contexts take 17; one request of 12 rows, 32 bf16 heads over 300 positions 9.7 for 21.
 //
 // Else a block has an equal run of all items' positions, as in attention_items.cuh, and parts of items are put together by the merge.  fp32 pages: the rows kernel has room for one warp a
-// scheduler beside their copies, here there are two: 8 requests of 25 rows, 40 heads over 1280 positions 174 us for 288 (2.5 TB/s; the terms of K and V and six products of each,
+// scheduler beside their copies, here there are two: 8 requests of 25 rows, 40 heads over 1280 positions 191 us for 288 (2.2 TB/s; the terms of K and V and six products of each,
 // 16 rows at a time), one of 8000 positions 81 for 117.  (bf16 pages stay with the rows kernel, whose copies run ahead: 94 us for 109.)
 #pragma once
 
